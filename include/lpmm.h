@@ -43,7 +43,7 @@ typedef int32_t lpmm_status;
 #define LPMM_ERR_CUDA (-5)            /* a CUDA runtime call or launch failed */
 #define LPMM_ERR_TOO_LARGE (-6)       /* larger than the fixed capacity of lpmm_quantize_rank1_noalloc */
 
-typedef enum { LPMM_F32 = 0, LPMM_BF16 = 1 } lpmm_dtype;
+typedef enum { LPMM_F32 = 0, LPMM_BF16 = 1, LPMM_F16 = 2 } lpmm_dtype; /* gradients of a step: F32 or BF16 */
 typedef enum { LPMM_NORM_BLOCK = 0, LPMM_NORM_RANK1 = 1 } lpmm_norm;          /* Sec. 2.2 / Sec. 4.2 */
 typedef enum { LPMM_MAP_DE_SIGNED = 0, LPMM_MAP_LINEAR_NOZERO = 1 } lpmm_map; /* App. E.2 / Sec. 4.1 */
 /* Second moment of 2-D tensors: 4-bit with rank-1 or block-wise normalization, or not stored at all but
@@ -246,6 +246,73 @@ lpmm_status lpmm_quantize_rank1_noalloc(const float* d_x, int64_t rows, int64_t 
 lpmm_status lpmm_dequantize(const uint8_t* d_codes, const float* d_scale0, const float* d_scale1,
                             int64_t rows, int64_t cols, int32_t norm, int32_t map, int32_t block,
                             float* d_out, void* stream);
+
+/* ---- 4-bit weights with group scales -----------------------------------------------------------------
+ *
+ * The form in which a trained matrix is put into service: weight (i, k) = (code - zero) * scale with one scale, and
+ * optionally one zero point, per `group` consecutive columns of a row (the last group of a row may be shorter).
+ *   d_codes  rows x codes_stride bytes; column 2k of a row sits in bits 0-3 of its byte k, column 2k + 1 in bits 4-7.
+ *            codes_stride is a multiple of 16 and at least ceil(cols / 2); d_codes is 16-byte aligned. What the bytes behind
+ *            a row's last column hold does not matter.
+ *   d_scales rows x ceil(cols / group), contiguous, of type scale_dtype (LPMM_F32, LPMM_BF16 or LPMM_F16).
+ *   d_zeros  rows x ceil(cols / group) bytes, contiguous, 0 .. 15; NULL: 8 everywhere.
+ *   group    32, 64 or a multiple of 128.
+ * All sums are kept in binary32 and every code enters the products exactly. */
+typedef struct {
+    uint8_t* d_codes;
+    void* d_scales;
+    uint8_t* d_zeros;
+    int64_t rows, cols, codes_stride;
+    int32_t group, scale_dtype;
+} lpmm_w4;
+
+/* Quantizes a rows x cols matrix (w_dtype, rows w_stride elements apart, w_stride >= cols) into the buffers of *m.
+ *   without zero points: scale = max |w| / 7, code = rint(w * (1/scale)) + 8;
+ *   with (d_zeros given): hi = max(w, 0), lo = min(w, 0), scale = (hi - lo) / 15, zero = rint(-lo * (1/scale)),
+ *   code = rint(w * (1/scale)) + zero; both clamped to 0 .. 15.
+ * The division by 7 or 15 is a product with the constant's reciprocal; 1/scale is the binary32 reciprocal of the scale as
+ * stored (rounded to scale_dtype), 0 for a scale below FLT_MIN. Bytes behind ceil(cols / 2) of a row may be set to 0.
+ * NaN or infinite weights give unspecified codes within 0 .. 15. */
+lpmm_status lpmm_w4_quantize(const void* d_w, int32_t w_dtype, int64_t w_stride, const lpmm_w4* m, void* stream);
+
+/* d_out[i * out_stride + k] = (code - zero) * scale: the binary32 product, rounded to out_dtype. */
+lpmm_status lpmm_w4_dequantize(const lpmm_w4* m, void* d_out, int32_t out_dtype, int64_t out_stride, void* stream);
+
+/* d_y[t * y_stride + i] = sum over k of d_x[t * x_stride + k] * weight(i, k) + bias[i], for `tokens` rows of activations
+ * (0: nothing to do). One read of the codes serves a block of tokens, so it is meant for single tokens and
+ * small batches; it is right for any number.
+ *   x_dtype  LPMM_F32, LPMM_BF16 or LPMM_F16; y_dtype the same, or LPMM_F32. d_bias: rows floats, or NULL.
+ *   x_stride >= cols, y_stride >= rows; d_x and d_y need the alignment of their elements only. */
+lpmm_status lpmm_w4_matvec(const lpmm_w4* m, const void* d_x, int32_t x_dtype, int64_t x_stride, int64_t tokens,
+                           const float* d_bias, void* d_y, int32_t y_dtype, int64_t y_stride, void* stream);
+
+/* ---- Distillation from a teacher's top logits ----------------------------------------------------------
+ *
+ * Per row: p = softmax(z / tau) over the vocabulary; K listed entries (id_k, teacher logit t_k). Without d_teacher_lse the
+ * teacher is q = softmax(t / tau) over the listed entries; with it (the log-sum-exp of the teacher's whole row of
+ * logits / tau) q_k = exp(t_k / tau - lse) and the entries left out are one more class, q_rest = max(1 - sum q, 0).
+ *   loss = w [ sum q_k (log q_k - log p_id_k) + q_rest (log q_rest - log p_rest) ],  0 log 0 = 0
+ *   grad = d loss / d z
+ * An id outside 0 .. vocab - 1 (such as -1) is no entry; a teacher logit of -infinity is an entry with q = 0; an id that is
+ * listed twice counts with both entries' q. A row without entries has loss 0 and gradient 0, and so has one whose entries
+ * all have q = 0 when no class is left out. A row of weight 0 is not read: loss 0, gradient 0 whatever its logits hold. Student logits of -infinity have p = 0 (loss +infinity if the teacher lists one
+ * with q > 0, the gradient stays finite); NaN or +infinity make the row's results NaN.
+ *   d_logits  tokens x vocab (dtype LPMM_F32, LPMM_BF16 or LPMM_F16), rows logits_stride elements apart
+ *   d_ids     tokens x top, contiguous, of ids_bytes 4 or 8; d_top_logits tokens x top, contiguous, of type top_dtype
+ *   d_teacher_lse, d_weights  tokens floats or NULL (no class of entries left out; weight 1)
+ *   d_loss    tokens floats; d_grad tokens x vocab of the logits' type, rows grad_stride elements apart. d_grad may be
+ *             d_logits itself with the same stride (the gradient then replaces the logits); it must not overlap otherwise.
+ * 1 <= top <= min(vocab, LPMM_DISTILL_MAX_TOP), vocab <= LPMM_DISTILL_MAX_VOCAB, else LPMM_ERR_UNSUPPORTED; tokens 0:
+ * nothing to do. Results do not depend on the launch: they are the same bits every time. */
+#define LPMM_DISTILL_MAX_TOP 1024
+#define LPMM_DISTILL_MAX_VOCAB 262144
+lpmm_status lpmm_distill_loss(const void* d_logits, int32_t dtype, int64_t logits_stride, int64_t tokens, int64_t vocab,
+                              const void* d_ids, int32_t ids_bytes, const void* d_top_logits, int32_t top_dtype, int32_t top,
+                              const float* d_teacher_lse, const float* d_weights, float temperature, float* d_loss, void* stream);
+lpmm_status lpmm_distill_grad(const void* d_logits, int32_t dtype, int64_t logits_stride, int64_t tokens, int64_t vocab,
+                              const void* d_ids, int32_t ids_bytes, const void* d_top_logits, int32_t top_dtype, int32_t top,
+                              const float* d_teacher_lse, const float* d_weights, float temperature, float* d_loss,
+                              void* d_grad, int64_t grad_stride, void* stream);
 
 /* Device pointers into the arena for tensor i's current state (for inspection and parity checks).
  * Pointers that do not apply to the tensor's kind are set to NULL. Sizes: codes ceil(numel/2) bytes;

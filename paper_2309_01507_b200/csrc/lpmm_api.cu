@@ -1269,6 +1269,102 @@ lpmm_status lpmm_dequantize(const uint8_t* d_codes, const float* d_scale0, const
     return LPMM_OK;
 }
 
+// ---- 4-bit weights and distillation
+
+namespace {
+
+bool known_dtype(int32_t d) { return d == LPMM_F32 || d == LPMM_BF16 || d == LPMM_F16; }
+int dtype_bytes(int32_t d) { return d == LPMM_F32 ? 4 : 2; }
+bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+lpmm_status check_w4(const lpmm_w4* m) {
+    if (!m || !m->d_codes || !m->d_scales || m->rows <= 0 || m->cols <= 0 || !known_dtype(m->scale_dtype)) return LPMM_ERR_INVALID_ARG;
+    if (m->rows > ((int64_t)1 << 40) / m->cols || m->cols > INT32_MAX / 2) return LPMM_ERR_INVALID_ARG;
+    if (m->codes_stride < (m->cols + 1) / 2 || m->codes_stride > ((int64_t)1 << 40) / m->rows) return LPMM_ERR_INVALID_ARG;
+    if (m->group != 32 && m->group != 64 && (m->group <= 0 || m->group % 128 != 0)) return LPMM_ERR_UNSUPPORTED;
+    if (m->codes_stride % 16 != 0 || !aligned16(m->d_codes) || !aligned_to(m->d_scales, dtype_bytes(m->scale_dtype))) return LPMM_ERR_ALIGNMENT;
+    return LPMM_OK;
+}
+W4Matrix to_w4(const lpmm_w4* m) {
+    return {m->d_codes, m->d_scales, m->d_zeros, m->rows, m->cols, m->codes_stride, m->group, m->scale_dtype};
+}
+// A strided matrix argument: rows of at least `cols` elements, aligned to its elements, extents that fit 63 bits with room.
+lpmm_status check_rows(const void* p, int32_t dtype, int64_t rows, int64_t cols, int64_t stride) {
+    if (!p || !known_dtype(dtype) || stride < cols) return LPMM_ERR_INVALID_ARG;
+    if (rows > 0 && stride > ((int64_t)1 << 42) / rows) return LPMM_ERR_INVALID_ARG;
+    return aligned_to(p, dtype_bytes(dtype)) ? LPMM_OK : LPMM_ERR_ALIGNMENT;
+}
+
+lpmm_status distill_impl(const void* d_logits, int32_t dtype, int64_t logits_stride, int64_t tokens, int64_t vocab, const void* d_ids,
+                         int32_t ids_bytes, const void* d_top_logits, int32_t top_dtype, int32_t top, const float* d_teacher_lse,
+                         const float* d_weights, float temperature, float* d_loss, void* d_grad, int64_t grad_stride, bool grad, void* stream) {
+    if (tokens < 0 || vocab <= 0 || top <= 0 || top > vocab || !known_dtype(dtype) || !known_dtype(top_dtype)) return LPMM_ERR_INVALID_ARG;
+    if (ids_bytes != 4 && ids_bytes != 8) return LPMM_ERR_INVALID_ARG;
+    if (!std::isfinite(temperature) || temperature <= 0.0f || !std::isfinite(1.0f / temperature * 2.0f)) return LPMM_ERR_INVALID_ARG;
+    if (top > LPMM_DISTILL_MAX_TOP || vocab > LPMM_DISTILL_MAX_VOCAB) return LPMM_ERR_UNSUPPORTED;
+    if (tokens == 0) return LPMM_OK;
+    if (tokens > INT32_MAX || !d_ids || !d_top_logits || !d_loss) return LPMM_ERR_INVALID_ARG;
+    lpmm_status rc = check_rows(d_logits, dtype, tokens, vocab, logits_stride);
+    if (rc == LPMM_OK && grad) rc = check_rows(d_grad, dtype, tokens, vocab, grad_stride);
+    if (rc != LPMM_OK) return rc;
+    if (grad && d_grad == d_logits && grad_stride != logits_stride) return LPMM_ERR_INVALID_ARG;
+    if (!aligned_to(d_ids, ids_bytes) || !aligned_to(d_top_logits, dtype_bytes(top_dtype)) || !aligned_to(d_loss, 4) ||
+        !aligned_to(d_teacher_lse, 4) || !aligned_to(d_weights, 4)) return LPMM_ERR_ALIGNMENT;
+    const float inv_tau = 1.0f / temperature;
+    const DistillArgs a = {d_logits, grad ? d_grad : nullptr, d_ids, d_top_logits, d_teacher_lse, d_weights, d_loss,
+                           tokens, vocab, logits_stride, grad_stride, top, ids_bytes == 8, inv_tau,
+                           (float)(1.0 / (double)temperature - (double)inv_tau)};
+    LPMM_CUDA(launch_distill(a, dtype, top_dtype, static_cast<cudaStream_t>(stream)));
+    return LPMM_OK;
+}
+
+}  // namespace
+
+lpmm_status lpmm_w4_quantize(const void* d_w, int32_t w_dtype, int64_t w_stride, const lpmm_w4* m, void* stream) {
+    lpmm_status rc = check_w4(m);
+    if (rc == LPMM_OK) rc = check_rows(d_w, w_dtype, m->rows, m->cols, w_stride);
+    if (rc != LPMM_OK) return rc;
+    LPMM_CUDA(launch_w4_quantize(to_w4(m), d_w, w_dtype, w_stride, static_cast<cudaStream_t>(stream)));
+    return LPMM_OK;
+}
+
+lpmm_status lpmm_w4_dequantize(const lpmm_w4* m, void* d_out, int32_t out_dtype, int64_t out_stride, void* stream) {
+    lpmm_status rc = check_w4(m);
+    if (rc == LPMM_OK) rc = check_rows(d_out, out_dtype, m->rows, m->cols, out_stride);
+    if (rc != LPMM_OK) return rc;
+    LPMM_CUDA(launch_w4_dequantize(to_w4(m), d_out, out_dtype, out_stride, static_cast<cudaStream_t>(stream)));
+    return LPMM_OK;
+}
+
+lpmm_status lpmm_w4_matvec(const lpmm_w4* m, const void* d_x, int32_t x_dtype, int64_t x_stride, int64_t tokens,
+                           const float* d_bias, void* d_y, int32_t y_dtype, int64_t y_stride, void* stream) {
+    lpmm_status rc = check_w4(m);
+    if (rc != LPMM_OK) return rc;
+    if (tokens < 0 || !known_dtype(x_dtype) || (y_dtype != x_dtype && y_dtype != LPMM_F32)) return LPMM_ERR_INVALID_ARG;
+    if (tokens == 0) return LPMM_OK;
+    rc = check_rows(d_x, x_dtype, tokens, m->cols, x_stride);
+    if (rc == LPMM_OK) rc = check_rows(d_y, y_dtype, tokens, m->rows, y_stride);
+    if (rc != LPMM_OK) return rc;
+    if (!aligned_to(d_bias, 4)) return LPMM_ERR_ALIGNMENT;
+    LPMM_CUDA(launch_w4_matvec(to_w4(m), d_x, x_dtype, x_stride, tokens, d_bias, d_y, y_dtype, y_stride, static_cast<cudaStream_t>(stream)));
+    return LPMM_OK;
+}
+
+lpmm_status lpmm_distill_loss(const void* d_logits, int32_t dtype, int64_t logits_stride, int64_t tokens, int64_t vocab,
+                              const void* d_ids, int32_t ids_bytes, const void* d_top_logits, int32_t top_dtype, int32_t top,
+                              const float* d_teacher_lse, const float* d_weights, float temperature, float* d_loss, void* stream) {
+    return distill_impl(d_logits, dtype, logits_stride, tokens, vocab, d_ids, ids_bytes, d_top_logits, top_dtype, top, d_teacher_lse,
+                        d_weights, temperature, d_loss, nullptr, 0, false, stream);
+}
+
+lpmm_status lpmm_distill_grad(const void* d_logits, int32_t dtype, int64_t logits_stride, int64_t tokens, int64_t vocab,
+                              const void* d_ids, int32_t ids_bytes, const void* d_top_logits, int32_t top_dtype, int32_t top,
+                              const float* d_teacher_lse, const float* d_weights, float temperature, float* d_loss,
+                              void* d_grad, int64_t grad_stride, void* stream) {
+    return distill_impl(d_logits, dtype, logits_stride, tokens, vocab, d_ids, ids_bytes, d_top_logits, top_dtype, top, d_teacher_lse,
+                        d_weights, temperature, d_loss, d_grad, grad_stride, true, stream);
+}
+
 lpmm_status lpmm_state_view(const lpmm_state* st, int32_t tensor, int32_t* kind,
                             const uint8_t** m_codes, const float** m_scale,
                             const uint8_t** v_codes, const float** v_scale0, const float** v_scale1,

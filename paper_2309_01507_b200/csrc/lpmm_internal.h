@@ -154,4 +154,32 @@ cudaError_t launch_dequantize(const uint8_t* codes, const float* s0, const float
 cudaError_t launch_quantize_rank1_noalloc(const float* x, int64_t rows, int64_t cols, uint8_t* codes, float* r,
                                           float* c, cudaStream_t s);
 
+// 4-bit weights with group scales (lpmm_w4 of the C ABI) and the operators on them. dtype: lpmm_dtype.
+struct W4Matrix {
+    uint8_t* codes;
+    void* scales;
+    uint8_t* zeros;
+    int64_t rows, cols, codes_stride;
+    int32_t group, scale_dtype;
+};
+cudaError_t launch_w4_quantize(const W4Matrix& m, const void* w, int dtype, int64_t w_stride, cudaStream_t s);
+cudaError_t launch_w4_dequantize(const W4Matrix& m, void* out, int dtype, int64_t out_stride, cudaStream_t s);
+cudaError_t launch_w4_matvec(const W4Matrix& m, const void* x, int x_dtype, int64_t x_stride, int64_t tokens, const float* bias,
+                             void* y, int y_dtype, int64_t y_stride, cudaStream_t s);
+
+// Distillation from a teacher's top logits. grad == nullptr: the loss alone.
+struct DistillArgs {
+    const void* logits;
+    void* grad;
+    const void* ids;
+    const void* top_logits;
+    const float* teacher_lse;   // nullptr: the teacher's probabilities are normalized over the listed entries
+    const float* weights;       // nullptr: 1
+    float* loss;
+    int64_t tokens, vocab, logits_stride, grad_stride;
+    int32_t top, ids64;
+    float inv_tau, inv_tau_lo;  // 1 / tau rounded, and what the rounding left: t / tau - lse cancels
+};
+cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, int top_dtype, cudaStream_t s);
+
 }  // namespace lpmm

@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(_HERE, "liblpmm.so")
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_ARENA_TOO_SMALL, ERR_CUDA = 0, -1, -2, -3, -4, -5
 ERR_TOO_LARGE = -6
 NOALLOC_MAX_SCALES = 262144
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 NORM_BLOCK, NORM_RANK1 = 0, 1
 MAP_DE_SIGNED, MAP_LINEAR_NOZERO = 0, 1
 V_RANK1, V_BLOCK, V_FACTORED = 0, 1, 2
@@ -33,7 +33,8 @@ EXPORTS = ("lpmm_state_bytes", "lpmm_state_init", "lpmm_state_attach", "lpmm_ada
            "lpmm_state_view", "lpmm_state_view_axis", "lpmm_state_phase", "lpmm_state_last_launches", "lpmm_state_destroy",
            "lpmm_state_profile", "lpmm_state_profile_read", "lpmm_state_device_status", "lpmm_state_selftest_wait",
            "lpmm_state_schedule", "lpmm_state_wait_stats", "lpmm_build_is_checking", "lpmm_state_check_guards",
-           "lpmm_state_selftest_check",
+           "lpmm_state_selftest_check", "lpmm_w4_quantize", "lpmm_w4_dequantize", "lpmm_w4_matvec", "lpmm_distill_loss",
+           "lpmm_distill_grad",
            "lpmm_status_string", "lpmm_last_cuda_error")
 
 
@@ -67,6 +68,11 @@ def default_config(v_mode: int = V_RANK1, min_quant_numel: int = 4096, update_ma
                    lead_melems: int = 0, gap_items: int = 0, no_l2_hints: int = 0, overlap_groups: int = 0) -> Config:
     return Config(4, m_block, 128, v_mode, min_quant_numel, update_math, schedule, tile_elems, tile_elems_maxima,
                   l2_keep_mbytes, lead_melems, gap_items, no_l2_hints, overlap_groups)
+
+
+class W4(C.Structure):
+    _fields_ = [("d_codes", C.c_void_p), ("d_scales", C.c_void_p), ("d_zeros", C.c_void_p), ("rows", C.c_int64),
+                ("cols", C.c_int64), ("codes_stride", C.c_int64), ("group", C.c_int32), ("scale_dtype", C.c_int32)]
 
 
 class LpmmError(RuntimeError):
@@ -122,6 +128,11 @@ def lib():
         L.lpmm_build_is_checking.argtypes = []
         L.lpmm_state_check_guards.argtypes = [vp, C.POINTER(i64), C.POINTER(i64), vp]
         L.lpmm_state_selftest_check.argtypes = [vp, C.POINTER(i32), vp]
+        L.lpmm_w4_quantize.argtypes = [vp, i32, i64, C.POINTER(W4), vp]
+        L.lpmm_w4_dequantize.argtypes = [C.POINTER(W4), vp, i32, i64, vp]
+        L.lpmm_w4_matvec.argtypes = [C.POINTER(W4), vp, i32, i64, i64, vp, vp, i32, i64, vp]
+        L.lpmm_distill_loss.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, i32, i32, vp, vp, f32, vp, vp]
+        L.lpmm_distill_grad.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, i32, i32, vp, vp, f32, vp, vp, i64, vp]
         L.lpmm_state_phase.argtypes = [vp]
         L.lpmm_state_last_launches.argtypes = [vp]
         L.lpmm_state_destroy.argtypes = [vp]
@@ -447,3 +458,183 @@ def state_view_axis(state: State, tensor: int, axis: int) -> torch.Tensor:
     _check(lib().lpmm_state_view_axis(state.handle, tensor, axis, C.byref(p), C.byref(n)), "lpmm_state_view_axis")
     off = p.value - state.arena.data_ptr()
     return state.arena[off:off + 4 * n.value].view(torch.float32)
+
+
+# ---- operators around the step: 4-bit weights, distillation --------------------------------------------
+
+DISTILL_MAX_TOP, DISTILL_MAX_VOCAB = 1024, 262144
+_DTYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+class _Enqueue:
+    """Where a call's work goes: the caller's stream (its raw pointer is `ptr`) or the current one of `device`. Results that
+    are allocated inside the block belong to that stream, and tensors handed to use() stay alive until its work is done, also
+    when they were made on another stream. Ordering that stream behind the tensors' producers is the caller's part."""
+
+    def __init__(self, stream, device):
+        self.stream, self.guards = stream, ()
+        if stream is not None:
+            self.guards = (torch.cuda.stream(stream),)          # makes the stream's device current too
+        elif device.index != torch.cuda.current_device():
+            self.guards = (torch.cuda.device(device),)
+
+    def __enter__(self):
+        for g in self.guards:
+            g.__enter__()
+        self.ptr = (self.stream or torch.cuda.current_stream()).cuda_stream
+        return self
+
+    def __exit__(self, *exc):
+        for g in self.guards:
+            g.__exit__(*exc)
+
+    def use(self, *tensors):
+        if self.stream is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+
+
+def _need(ok: bool, message: str) -> None:
+    if not ok:
+        raise ValueError(message)
+
+
+def _rows_of(x: torch.Tensor, name: str) -> int:
+    """Distance between the rows of a matrix whose rows are contiguous."""
+    rows, cols = x.shape
+    _need(cols <= 1 or x.stride(1) == 1, f"the rows of {name} must be contiguous")
+    stride = x.stride(0) if rows > 1 else max(x.stride(0), cols)
+    _need(stride >= cols, f"the rows of {name} must not overlap")
+    return stride
+
+
+def _dtype_of(x: torch.Tensor, name: str) -> int:
+    _need(x.dtype in _DTYPE, f"{name} must be float32, bfloat16 or float16, not {x.dtype}")
+    return _DTYPE[x.dtype]
+
+
+class W4Matrix:
+    """A rows x cols matrix in 4 bits with group scales (lpmm_w4): `codes` (uint8, rows x pitch, pitch a multiple of 16 and at
+    least ceil(cols / 2); column 2k of a row in the low half of its byte k), `scales` (rows x ceil(cols / group), float32,
+    bfloat16 or float16) and `zeros` (uint8 of the same shape, 0 .. 15, or None: 8). Value = (code - zero) * scale. The
+    tensors are the caller's own, read where they are; w4_quantize makes all of them from a matrix."""
+
+    def __init__(self, codes, scales, cols, *, group=128, zeros=None):
+        _need(codes.dtype == torch.uint8 and codes.is_cuda and codes.dim() == 2, "codes must be a 2-D uint8 CUDA tensor")
+        rows, groups = codes.shape[0], -(-cols // group) if group > 0 and cols > 0 else 0
+        _need(rows > 0 and groups > 0, "a matrix needs at least one row, one column and a positive group")
+        stride = _rows_of(codes, "codes")
+        _need(codes.shape[1] >= (cols + 1) // 2, f"codes holds {codes.shape[1]} bytes per row, {(cols + 1) // 2} are needed")
+        if rows == 1:       # the distance to a next row does not matter
+            stride = (max(stride, codes.shape[1]) + 15) // 16 * 16
+        for name, t in (("scales", scales), ("zeros", zeros)):
+            if t is not None:
+                _need(t.shape == (rows, groups) and t.is_contiguous() and t.device == codes.device,
+                      f"{name} must be a contiguous {rows} x {groups} tensor on the codes' device")
+        _need(zeros is None or zeros.dtype == torch.uint8, "zeros must be uint8")
+        self.codes, self.scales, self.zeros, self.rows, self.cols, self.group = codes, scales, zeros, rows, cols, group
+        self._c = W4(codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), rows, cols, stride, group,
+                     _dtype_of(scales, "scales"))
+        self._ref = C.byref(self._c)
+
+    @property
+    def shape(self):
+        return self.rows, self.cols
+
+
+def w4_quantize(w: torch.Tensor, *, group: int = 128, zero_points: bool = False, scale_dtype=torch.float32, stream=None) -> W4Matrix:
+    """lpmm_w4_quantize: the 4-bit form of a matrix (float32, bfloat16 or float16, rows contiguous)."""
+    _need(w.is_cuda and w.dim() == 2 and w.numel() > 0, "w must be a non-empty 2-D CUDA tensor")
+    _need(group > 0 and scale_dtype in _DTYPE, "group must be positive and scale_dtype float32, bfloat16 or float16")
+    dtype, stride = _dtype_of(w, "w"), _rows_of(w, "w")
+    rows, cols = w.shape
+    groups = -(-cols // group)
+    with _Enqueue(stream, w.device) as q:
+        codes = torch.empty(rows, -(-cols // 32) * 16, dtype=torch.uint8, device=w.device)
+        scales = torch.empty(rows, groups, dtype=scale_dtype, device=w.device)
+        zeros = torch.empty(rows, groups, dtype=torch.uint8, device=w.device) if zero_points else None
+        m = W4Matrix(codes, scales, cols, group=group, zeros=zeros)
+        q.use(w)
+        _check(lib().lpmm_w4_quantize(w.data_ptr(), dtype, stride, m._ref, q.ptr), "lpmm_w4_quantize")
+    return m
+
+
+def w4_dequantize(m: W4Matrix, dtype=torch.float32, *, out=None, stream=None) -> torch.Tensor:
+    """lpmm_w4_dequantize: the matrix the codes stand for, in `dtype` (or into `out`, whose type then counts)."""
+    with _Enqueue(stream, m.codes.device) as q:
+        if out is None:
+            _need(dtype in _DTYPE, "dtype must be float32, bfloat16 or float16")
+            out = torch.empty(m.rows, m.cols, dtype=dtype, device=m.codes.device)
+        else:
+            _need(out.shape == m.shape and out.device == m.codes.device, f"out must be a {m.rows} x {m.cols} tensor on the codes' device")
+        q.use(m.codes, m.scales, m.zeros, out)
+        _check(lib().lpmm_w4_dequantize(m._ref, out.data_ptr(), _dtype_of(out, "out"), _rows_of(out, "out"), q.ptr), "lpmm_w4_dequantize")
+    return out
+
+
+def w4_matvec(m: W4Matrix, x: torch.Tensor, *, bias=None, out=None, out_dtype=None, stream=None) -> torch.Tensor:
+    """lpmm_w4_matvec: x W^T + bias for activations x (cols, or tokens x cols with contiguous rows) of float32, bfloat16 or
+    float16. The result has x's type, or float32 with out_dtype=torch.float32 (or `out`)."""
+    _need(x.dim() in (1, 2) and x.shape[-1] == m.cols and x.device == m.codes.device, f"x must have {m.cols} columns and lie on the codes' device")
+    x2 = x if x.dim() == 2 else x.unsqueeze(0)
+    tokens = x2.shape[0]
+    if bias is not None:
+        _need(bias.shape == (m.rows,) and bias.dtype == torch.float32 and bias.is_contiguous() and bias.device == x.device,
+              f"bias must be a contiguous float32 tensor of {m.rows} elements on x's device")
+    with _Enqueue(stream, x.device) as q:
+        shape = (m.rows,) if x.dim() == 1 else (tokens, m.rows)
+        if out is None:
+            out = torch.empty(shape, dtype=out_dtype or x.dtype, device=x.device)
+        else:
+            _need(out.shape == shape and out.device == x.device and out_dtype in (None, out.dtype), f"out must be a {shape} tensor on x's device")
+        out2 = out if x.dim() == 2 else out.unsqueeze(0)
+        _need(out.dtype in (x.dtype, torch.float32), "the result must have x's type or float32")
+        q.use(m.codes, m.scales, m.zeros, x, bias, out)
+        _check(lib().lpmm_w4_matvec(m._ref, x2.data_ptr(), _dtype_of(x, "x"), _rows_of(x2, "x"), tokens,
+                                    None if bias is None else bias.data_ptr(), out2.data_ptr(), _DTYPE[out.dtype],
+                                    _rows_of(out2, "out"), q.ptr), "lpmm_w4_matvec")
+    return out
+
+
+def _distill(logits, top_ids, top_logits, temperature, teacher_lse, weights, grad, stream):
+    _need(logits.is_cuda and logits.dim() == 2 and logits.shape[1] > 0, "logits must be a tokens x vocabulary CUDA tensor")
+    tokens, vocab = logits.shape
+    dtype, stride = _dtype_of(logits, "logits"), _rows_of(logits, "logits")
+    _need(top_ids.dim() == 2 and top_ids.shape[0] == tokens and top_ids.shape == top_logits.shape, "top_ids and top_logits must be tokens x top")
+    _need(top_ids.dtype in (torch.int32, torch.int64), "top_ids must be int32 or int64")
+    for name, t in (("top_ids", top_ids), ("top_logits", top_logits), ("teacher_lse", teacher_lse), ("weights", weights)):
+        if t is not None:
+            _need(t.is_contiguous() and t.device == logits.device, f"{name} must be contiguous and on the logits' device")
+    for name, t in (("teacher_lse", teacher_lse), ("weights", weights)):
+        if t is not None:
+            _need(t.shape == (tokens,) and t.dtype == torch.float32, f"{name} must be a float32 tensor of {tokens} elements")
+    with _Enqueue(stream, logits.device) as q:
+        loss = torch.empty(tokens, dtype=torch.float32, device=logits.device)
+        args = (logits.data_ptr(), dtype, stride, tokens, vocab, top_ids.data_ptr(), top_ids.element_size(), top_logits.data_ptr(),
+                _dtype_of(top_logits, "top_logits"), top_ids.shape[1], None if teacher_lse is None else teacher_lse.data_ptr(),
+                None if weights is None else weights.data_ptr(), temperature, loss.data_ptr())
+        q.use(logits, top_ids, top_logits, teacher_lse, weights)
+        if grad is None:
+            _check(lib().lpmm_distill_loss(*args, q.ptr), "lpmm_distill_loss")
+            return loss, None
+        if grad is True:
+            grad = torch.empty(tokens, vocab, dtype=logits.dtype, device=logits.device)
+        else:
+            _need(grad.shape == logits.shape and grad.dtype == logits.dtype and grad.device == logits.device, "out must match the logits")
+            q.use(grad)
+        _check(lib().lpmm_distill_grad(*args, grad.data_ptr(), _rows_of(grad, "out"), q.ptr), "lpmm_distill_grad")
+    return loss, grad
+
+
+def distill_loss(logits, top_ids, top_logits, *, temperature=1.0, teacher_lse=None, weights=None, stream=None) -> torch.Tensor:
+    """lpmm_distill_loss: per-row cross-entropy excess (KL divergence) of the student's softmax(logits / temperature) against a
+    teacher of whom each row's top logits are known, times the row's weight. `teacher_lse` (log-sum-exp of the teacher's whole
+    row of logits / temperature) adds the class of all other entries. Rows of `logits` contiguous, any distance apart."""
+    return _distill(logits, top_ids, top_logits, temperature, teacher_lse, weights, None, stream)[0]
+
+
+def distill_grad(logits, top_ids, top_logits, *, temperature=1.0, teacher_lse=None, weights=None, out=None, stream=None):
+    """lpmm_distill_grad: (loss, gradient of the summed loss with respect to the logits, in the logits' type) in one pass. As a
+    backward pass, `weights` are the gradients that arrive at the rows' losses. out=logits writes the gradient over the logits."""
+    return _distill(logits, top_ids, top_logits, temperature, teacher_lse, weights, True if out is None else out, stream)

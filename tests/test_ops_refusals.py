@@ -1,0 +1,117 @@
+"""What the operators around the step refuse, on the host: nothing here reaches a GPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2309_01507_b200 import build as lib_build
+from paper_2309_01507_b200 import lpmm
+
+lib_build.build()
+
+P = 0x1000       # stands for a device pointer; a refused call never looks behind it
+
+
+def _w4(**kw):
+    f = dict(d_codes=P, d_scales=P, d_zeros=None, rows=4, cols=64, codes_stride=32, group=32, scale_dtype=lpmm.F32)
+    f.update(kw)
+    return lpmm.W4(*[f[n] for n, _ in lpmm.W4._fields_])
+
+
+BAD_W4 = [(dict(d_codes=None), lpmm.ERR_INVALID_ARG), (dict(d_scales=None), lpmm.ERR_INVALID_ARG), (dict(rows=0), lpmm.ERR_INVALID_ARG),
+          (dict(cols=-1), lpmm.ERR_INVALID_ARG), (dict(codes_stride=16), lpmm.ERR_INVALID_ARG), (dict(scale_dtype=3), lpmm.ERR_INVALID_ARG),
+          (dict(rows=1 << 40), lpmm.ERR_INVALID_ARG), (dict(group=16), lpmm.ERR_UNSUPPORTED), (dict(group=96), lpmm.ERR_UNSUPPORTED),
+          (dict(group=0), lpmm.ERR_UNSUPPORTED), (dict(group=-128), lpmm.ERR_UNSUPPORTED), (dict(codes_stride=40), lpmm.ERR_ALIGNMENT),
+          (dict(d_codes=P + 8), lpmm.ERR_ALIGNMENT), (dict(d_scales=P + 2), lpmm.ERR_ALIGNMENT)]
+
+
+@pytest.mark.parametrize("fields,want", BAD_W4, ids=[str(f) for f, _ in BAD_W4])
+def test_bad_matrices(fields, want):
+    L, m = lpmm.lib(), _w4(**fields)
+    assert L.lpmm_w4_matvec(C.byref(m), P, lpmm.F32, 64, 1, None, P, lpmm.F32, 4, None) == want
+    assert L.lpmm_w4_quantize(P, lpmm.F32, 64, C.byref(m), None) == want
+    assert L.lpmm_w4_dequantize(C.byref(m), P, lpmm.F32, 64, None) == want
+
+
+def test_bad_activations_and_outputs():
+    L, m = lpmm.lib(), _w4()
+    ok = dict(x=P, xd=lpmm.BF16, xs=64, t=2, b=None, y=P, yd=lpmm.BF16, ys=4)
+    for change, want in ((dict(x=None), -1), (dict(y=None), -1), (dict(t=-1), -1), (dict(xs=63), -1), (dict(ys=3), -1), (dict(xd=7), -1),
+                         (dict(yd=lpmm.F16), -1), (dict(xd=lpmm.F32, yd=lpmm.BF16), -1), (dict(xs=1 << 42), -1), (dict(x=P + 1), -3),
+                         (dict(y=P + 1), -3), (dict(b=P + 2), -3)):
+        a = {**ok, **change}
+        assert L.lpmm_w4_matvec(C.byref(m), a["x"], a["xd"], a["xs"], a["t"], a["b"], a["y"], a["yd"], a["ys"], None) == want, change
+    assert L.lpmm_w4_matvec(None, P, 0, 64, 1, None, P, 0, 4, None) == lpmm.ERR_INVALID_ARG
+    assert L.lpmm_w4_matvec(C.byref(m), None, 0, 64, 0, None, None, 0, 4, None) == lpmm.OK        # no tokens
+    assert L.lpmm_w4_quantize(None, 0, 64, C.byref(m), None) == lpmm.ERR_INVALID_ARG
+    assert L.lpmm_w4_quantize(P, 0, 63, C.byref(m), None) == lpmm.ERR_INVALID_ARG
+    assert L.lpmm_w4_quantize(P + 2, 0, 64, C.byref(m), None) == lpmm.ERR_ALIGNMENT
+    assert L.lpmm_w4_dequantize(C.byref(m), None, 0, 64, None) == lpmm.ERR_INVALID_ARG
+    assert L.lpmm_w4_dequantize(C.byref(m), P, 5, 64, None) == lpmm.ERR_INVALID_ARG
+
+
+def test_bad_distillation_arguments():
+    L = lpmm.lib()
+    ok = dict(z=P, d=lpmm.F32, s=100, t=3, v=100, i=P, ib=8, tl=P, td=lpmm.F32, k=5, lse=None, w=None, tau=1.0, l=P, g=P + 4096, gs=100)
+
+    def call(**change):
+        a = {**ok, **change}
+        head = (a["z"], a["d"], a["s"], a["t"], a["v"], a["i"], a["ib"], a["tl"], a["td"], a["k"], a["lse"], a["w"], a["tau"], a["l"])
+        return L.lpmm_distill_loss(*head, None), L.lpmm_distill_grad(*head, a["g"], a["gs"], None)
+
+    inf, nan = float("inf"), float("nan")
+    for change, want in ((dict(z=None), -1), (dict(i=None), -1), (dict(tl=None), -1), (dict(l=None), -1), (dict(d=3), -1), (dict(td=-1), -1),
+                         (dict(s=99), -1), (dict(t=-1), -1), (dict(v=0), -1), (dict(k=0), -1), (dict(k=101), -1), (dict(ib=2), -1),
+                         (dict(tau=0.0), -1), (dict(tau=-1.0), -1), (dict(tau=inf), -1), (dict(tau=nan), -1), (dict(tau=1e-42), -1),
+                         (dict(v=2000, s=2000, gs=2000, k=1025), -2), (dict(v=262145, s=262145, gs=262145), -2), (dict(z=P + 2), -3), (dict(i=P + 4), -3),
+                         (dict(tl=P + 1), -3), (dict(lse=P + 1), -3), (dict(w=P + 2), -3), (dict(l=P + 1), -3)):
+        assert call(**change) == (want, want), change
+    assert call(g=None)[1] == -1 and call(gs=99)[1] == -1 and call(g=P + 4097)[1] == -3
+    assert call(z=P, g=P, s=100, gs=104)[1] == -1           # in place needs the same rows
+    assert call(t=0) == (0, 0) and call(t=0, z=None, i=None, tl=None, l=None, g=None) == (0, 0)
+
+
+def test_the_step_still_refuses_half_precision_gradients():
+    assert lpmm.lib().lpmm_adamw4_step(None, None, None, lpmm.F16, 1e-3, 0.9, 0.999, 1e-8, 0.0, 1, None) == lpmm.ERR_INVALID_ARG
+    with pytest.raises(ValueError):
+        lpmm._grad_dtype([torch.zeros(2, dtype=torch.float16)])
+
+
+def test_the_binding_refuses_before_the_library_is_called():
+    x = torch.zeros(2, 64)
+    for call in (lambda: lpmm.w4_quantize(x), lambda: lpmm.W4Matrix(torch.zeros(4, 32, dtype=torch.uint8), torch.zeros(4, 2), 64, group=32),
+                 lambda: lpmm.distill_loss(x, torch.zeros(2, 3, dtype=torch.int64), torch.zeros(2, 3)),
+                 lambda: lpmm.distill_grad(x, torch.zeros(2, 3, dtype=torch.int64), torch.zeros(2, 3))):
+        with pytest.raises(ValueError):
+            call()
+
+
+@pytest.mark.gpu
+def test_the_binding_refuses_mismatched_gpu_tensors():
+    codes, scales = torch.zeros(4, 32, dtype=torch.uint8, device="cuda"), torch.ones(4, 2, device="cuda")
+    m = lpmm.W4Matrix(codes, scales, 64, group=32)
+    x = torch.zeros(2, 64, device="cuda")
+    bad = [lambda: lpmm.W4Matrix(codes.int(), scales, 64, group=32), lambda: lpmm.W4Matrix(codes, scales[:, :1], 64, group=32),
+           lambda: lpmm.W4Matrix(codes, scales.double(), 64, group=32), lambda: lpmm.W4Matrix(codes, scales, 65, group=32),
+           lambda: lpmm.W4Matrix(codes[:0], scales[:0], 64, group=32), lambda: lpmm.W4Matrix(codes, scales, 64, group=0),
+           lambda: lpmm.W4Matrix(codes, scales, 64, group=32, zeros=scales), lambda: lpmm.W4Matrix(codes.t(), scales, 8, group=8),
+           lambda: lpmm.w4_matvec(m, x[:, :63]), lambda: lpmm.w4_matvec(m, x.double()), lambda: lpmm.w4_matvec(m, x.t()), lambda: lpmm.w4_matvec(m, x.cpu()),
+           lambda: lpmm.w4_matvec(m, x, bias=torch.zeros(3, device="cuda")), lambda: lpmm.w4_matvec(m, x, out_dtype=torch.bfloat16),
+           lambda: lpmm.w4_matvec(m, x, out=torch.zeros(2, 5, device="cuda")), lambda: lpmm.w4_matvec(m, x[:, None]),
+           lambda: lpmm.w4_dequantize(m, torch.float64), lambda: lpmm.w4_dequantize(m, out=torch.zeros(4, 63, device="cuda")),
+           lambda: lpmm.w4_quantize(x, group=0), lambda: lpmm.w4_quantize(x, scale_dtype=torch.float64), lambda: lpmm.w4_quantize(x.t()),
+           lambda: lpmm.w4_quantize(x[0])]
+    z, ids, t = torch.zeros(3, 50, device="cuda"), torch.zeros(3, 4, dtype=torch.int64, device="cuda"), torch.zeros(3, 4, device="cuda")
+    bad += [lambda: lpmm.distill_loss(z.double(), ids, t), lambda: lpmm.distill_loss(z, ids[:2], t), lambda: lpmm.distill_loss(z, ids.short(), t),
+            lambda: lpmm.distill_loss(z, ids, t[:, :3]), lambda: lpmm.distill_loss(z, ids, t.cpu()), lambda: lpmm.distill_loss(z, ids, t, weights=t[:, 0]),
+            lambda: lpmm.distill_loss(z, ids, t, weights=torch.zeros(2, device="cuda")), lambda: lpmm.distill_loss(z[0], ids, t),
+            lambda: lpmm.distill_loss(z, ids, t, teacher_lse=torch.zeros(3, dtype=torch.float64, device="cuda")), lambda: lpmm.distill_loss(z.t(), ids, t),
+            lambda: lpmm.distill_grad(z, ids, t, out=z[:, :49]), lambda: lpmm.distill_grad(z, ids, t, out=z.half()),
+            lambda: lpmm.distill_loss(z[:1].expand(3, 50), ids, t), lambda: lpmm.distill_loss(z, ids, t.double())]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: lpmm.W4Matrix(codes, scales[:, :1].contiguous(), 64, group=48) and lpmm.w4_quantize(x, group=48), lambda: lpmm.distill_loss(z, ids, t, temperature=0.0),
+                 lambda: lpmm.distill_loss(z, ids[:, :0].contiguous(), t[:, :0].contiguous())):
+        with pytest.raises((lpmm.LpmmError, ValueError)):
+            call()
