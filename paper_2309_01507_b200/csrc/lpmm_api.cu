@@ -1312,9 +1312,9 @@ lpmm_status distill_impl(const void* d_logits, int32_t dtype, int64_t logits_str
         !aligned_to(d_teacher_lse, 4) || !aligned_to(d_weights, 4)) return LPMM_ERR_ALIGNMENT;
     const float inv_tau = 1.0f / temperature;
     const DistillArgs a = {d_logits, grad ? d_grad : nullptr, d_ids, d_top_logits, d_teacher_lse, d_weights, d_loss,
-                           tokens, vocab, logits_stride, grad_stride, top, ids_bytes == 8, inv_tau,
+                           tokens, vocab, logits_stride, grad_stride, top, ids_bytes == 8, top_dtype, inv_tau,
                            (float)(1.0 / (double)temperature - (double)inv_tau)};
-    LPMM_CUDA(launch_distill(a, dtype, top_dtype, static_cast<cudaStream_t>(stream)));
+    LPMM_CUDA(launch_distill(a, dtype, static_cast<cudaStream_t>(stream)));
     return LPMM_OK;
 }
 

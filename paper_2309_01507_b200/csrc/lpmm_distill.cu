@@ -107,8 +107,8 @@ enum { P_MREST, P_SREST, P_MTOP, P_STOP, P_NTOP, P_COUNT };   // what warps, and
 // One cluster of CTAs per row of logits, each CTA a slice of whole 16-byte vectors of it, which it holds in shared memory: the
 // row is read from HBM once, and the gradient written once. Every thread copies, reduces and writes the same vectors, so that
 // only the listed entries, which are taken out of the slice (set to -infinity), need barriers.
-template <typename T, typename U, int THREADS, bool GRAD>
-__global__ void __launch_bounds__(THREADS) distill_kernel(const DistillArgs a, const int cluster, const int slice_vecs) {
+template <typename T, int THREADS, bool GRAD>
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const DistillArgs a, const int cluster, const int slice_vecs) {
     using Bits = typename Row<T>::Bits;
     constexpr int VE = Row<T>::n, WARPS = THREADS / 32;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(THREADS) distill_kernel(const DistillArgs a, c
             for (int k = lane; k < K; k += 32) {
                 const int64_t id = a.ids64 ? static_cast<const int64_t*>(a.ids)[t * K + k] : static_cast<const int32_t*>(a.ids)[t * K + k];
                 const bool ok = id >= 0 && id < V;
-                const float tl = ok ? to_f32(static_cast<const U*>(a.top_logits)[t * K + k]) : -INFINITY;
+                const float tl = ok ? load_f32(a.top_logits, a.top_dtype, t * K + k) : -INFINITY;
                 ids[k] = ok ? (int)id : -1;
                 lq[k] = tl;
                 tmax = fmaxf(tmax, tl);
@@ -221,12 +221,14 @@ __global__ void __launch_bounds__(THREADS) distill_kernel(const DistillArgs a, c
             n_top = warp_sum(n_top);
         }
         VecMax<T> vm;
+#pragma unroll 4
         for (int v = tid; v < v1 - v0; v += THREADS) vm.add(vec[v]);
         float m_rest = warp_max1(vm.value()), s_rest = 0.0f;
         {
             const float ref = finite_ref(m_rest);
             const float2 neg = splat(-ref), c2 = splat(c);
             float2 sum = splat(0.0f);
+#pragma unroll 2
             for (int v = tid; v < v1 - v0; v += THREADS) {
                 float2 x[VE / 2];
                 to_pairs<T>(vec[v], x);
@@ -289,6 +291,7 @@ __global__ void __launch_bounds__(THREADS) distill_kernel(const DistillArgs a, c
             const float coef = (Q * f_rest * inv_s - (s_rest > 0.0f ? q_rest / s_rest : 0.0f)) * scale;
             const float2 neg = splat(-finite_ref(m_rest)), c2 = splat(c), coef2 = splat(coef);
             if ((reinterpret_cast<uintptr_t>(g) - reinterpret_cast<uintptr_t>(z)) % 16 == 0) {
+#pragma unroll 1
                 for (int v = tid; v < v1 - v0; v += THREADS) {
                     float2 x[VE / 2];
                     to_pairs<T>(vec[v], x);
@@ -310,6 +313,7 @@ __global__ void __launch_bounds__(THREADS) distill_kernel(const DistillArgs a, c
                 // The gradient's rows are aligned otherwise than the logits': its own vectors, gathered element by element.
                 const int goff = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T));
                 const int u1 = (j1 + goff + VE - 1) / VE;
+#pragma unroll 1
                 for (int u = (j0 + goff) / VE + tid; u < u1; u += THREADS) {
                     const int j = u * VE - goff;
                     float2 x[VE / 2];
@@ -365,9 +369,9 @@ __global__ void __launch_bounds__(THREADS) distill_kernel(const DistillArgs a, c
     }
 }
 
-template <typename T, typename U, int THREADS, bool GRAD>
+template <typename T, int THREADS, bool GRAD>
 cudaError_t launch(const DistillArgs& a, int cluster, int slice_vecs, size_t bytes, cudaStream_t s) {
-    auto kernel = distill_kernel<T, U, THREADS, GRAD>;
+    auto kernel = distill_kernel<T, THREADS, GRAD>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != cudaSuccess) return e;
     const int64_t rows = a.tokens < (1 << 24) ? a.tokens : 1 << 24;
@@ -388,7 +392,7 @@ cudaError_t launch(const DistillArgs& a, int cluster, int slice_vecs, size_t byt
 
 }  // namespace
 
-cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, int top_dtype, cudaStream_t s) {
+cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, cudaStream_t s) {
     const int64_t es = logits_dtype == 0 ? 4 : 2;
     const int64_t row_vecs = a.vocab * es / 16 + 2;    // however the row is aligned
     // Slices of up to 64 KB, three of which an SM holds at a time; eight CTAs at most. Few rows are split further, until every
@@ -399,12 +403,9 @@ cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, int top_dtype
     const int slice = (int)((row_vecs + cluster - 1) / cluster) + 1;
     const size_t bytes = (size_t)slice * 16 + (size_t)a.top * 12;
     return with_dtype(logits_dtype, [&](auto t) {
-        return with_dtype(top_dtype, [&](auto u) {
-            using T = decltype(t);
-            using U = decltype(u);
-            if (slice <= 1024) return a.grad ? launch<T, U, 128, true>(a, cluster, slice, bytes, s) : launch<T, U, 128, false>(a, cluster, slice, bytes, s);
-            return a.grad ? launch<T, U, 512, true>(a, cluster, slice, bytes, s) : launch<T, U, 512, false>(a, cluster, slice, bytes, s);
-        });
+        using T = decltype(t);
+        if (slice <= 1024) return a.grad ? launch<T, 128, true>(a, cluster, slice, bytes, s) : launch<T, 128, false>(a, cluster, slice, bytes, s);
+        return a.grad ? launch<T, 512, true>(a, cluster, slice, bytes, s) : launch<T, 512, false>(a, cluster, slice, bytes, s);
     });
 }
 

@@ -177,9 +177,9 @@ struct DistillArgs {
     const float* weights;       // nullptr: 1
     float* loss;
     int64_t tokens, vocab, logits_stride, grad_stride;
-    int32_t top, ids64;
+    int32_t top, ids64, top_dtype;
     float inv_tau, inv_tau_lo;  // 1 / tau rounded, and what the rounding left: t / tau - lse cancels
 };
-cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, int top_dtype, cudaStream_t s);
+cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, cudaStream_t s);
 
 }  // namespace lpmm

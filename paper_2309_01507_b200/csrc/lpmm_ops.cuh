@@ -17,6 +17,13 @@ template <> __device__ __forceinline__ float from_f32<float>(float x) { return x
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 
+// Element i of an array whose type is known at run time only.
+__device__ __forceinline__ float load_f32(const void* p, int dtype, int64_t i) {
+    if (dtype == 0) return static_cast<const float*>(p)[i];
+    if (dtype == 1) return to_f32(static_cast<const __nv_bfloat16*>(p)[i]);
+    return to_f32(static_cast<const __half*>(p)[i]);
+}
+
 // Two 16-bit elements as one 32-bit word, element 0 in the low half.
 template <typename T> __device__ __forceinline__ uint32_t pack_pair(float a, float b);
 template <> __device__ __forceinline__ uint32_t pack_pair<__nv_bfloat16>(float a, float b) {
