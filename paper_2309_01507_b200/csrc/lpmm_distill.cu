@@ -9,6 +9,8 @@
 // Powers are taken in base 2 of c (z_j - max z), c = log2(e) / tau: the difference first, so that logits masked with the type's
 // lowest value cannot overflow. p_rest is summed over the entries left out themselves, relative to their own maximum, never
 // taken as 1 - sum p: it keeps its precision, and its logarithm, when the student is sure of the listed entries.
+#include <algorithm>
+
 #include "lpmm_internal.h"
 #include "lpmm_ops.cuh"
 
@@ -104,59 +106,74 @@ __device__ __forceinline__ float2 join_lanes(float m, float s, float c) {
 
 enum { P_MREST, P_SREST, P_MTOP, P_STOP, P_NTOP, P_COUNT };   // what warps, and then CTAs of a cluster, exchange
 
+// What one warp works out for a row and all others read.
+struct RowResult {
+    float ref, coef;           // left out: gradient = coef 2^(c (z - ref))
+    float m, q_scale, scale;   // listed: q_scale 2^(c (z - m)) - q scale
+};
+
 // One cluster of CTAs per row of logits, each CTA a slice of whole 16-byte vectors of it, which it holds in shared memory: the
 // row is read from HBM once, and the gradient written once. Every thread copies, reduces and writes the same vectors, so that
-// only the listed entries, which are taken out of the slice (set to -infinity), need barriers.
+// only the listed entries, which are taken out of the slice (set to -infinity), need barriers. The first `entry_warps` warps
+// take the listed entries, warp 0 the teacher and what is worked out once per row.
 template <typename T, int THREADS, bool GRAD>
-__global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const DistillArgs a, const int cluster, const int slice_vecs) {
+__global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const DistillArgs a, const int log_cluster, const int slice_vecs, const int entry_warps) {
     using Bits = typename Row<T>::Bits;
     constexpr int VE = Row<T>::n, WARPS = THREADS / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     uint4* const vec = reinterpret_cast<uint4*>(smem);
     Bits* const elem = reinterpret_cast<Bits*>(smem);
-    int* const ids = reinterpret_cast<int*>(vec + slice_vecs);   // K ids, -1: no entry
-    float* const lq = reinterpret_cast<float*>(ids + a.top);     // logarithms of the teacher's probabilities (see log_t)
-    float* const zk = lq + a.top;                                // the student's logits at the ids of this slice
-    __shared__ float part[WARPS][P_COUNT], loss_part[WARPS], teacher[2];
-    __shared__ float ranks[kMaxCluster][P_COUNT], loss_ranks[kMaxCluster];
-    const int K = a.top, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int rank = cluster > 1 ? (int)cluster_rank() : 0;
+    int* const slot = reinterpret_cast<int*>(vec + slice_vecs);   // K ids, later the element in the slice; -1: no entry here
+    float* const lq = reinterpret_cast<float*>(slot + a.top);     // logarithms of the teacher's probabilities
+    float* const zk = lq + a.top;                                 // the student's logits at the ids of this slice
+    __shared__ float part[WARPS][P_COUNT], top_part[WARPS][2];
+    __shared__ float ranks[kMaxCluster][P_COUNT + 2];
+    __shared__ RowResult result;
+    const int K = a.top, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, estride = entry_warps * 32;
+    const int cluster = 1 << log_cluster, rank = log_cluster ? (int)cluster_rank() : 0;
     const float c = a.inv_tau * kLog2e;
-    const bool tail = a.teacher_lse != nullptr;
-    if (cluster > 1) cluster_barrier();       // every CTA is there before another stores into its shared memory
+    const bool tail = a.teacher_lse != nullptr, entries = warp < entry_warps;
+    if (log_cluster) cluster_barrier();       // every CTA is there before another stores into its shared memory
 
-    for (int64_t t = blockIdx.x / cluster; t < a.tokens; t += gridDim.x / cluster) {
+    for (int64_t t = blockIdx.x >> log_cluster; t < a.tokens; t += gridDim.x >> log_cluster) {
         const float w = a.weights ? a.weights[t] : 1.0f;
         const T* const z = static_cast<const T*>(a.logits) + t * a.logits_stride;
         T* const g = GRAD ? static_cast<T*>(a.grad) + t * a.grad_stride : nullptr;
         // The row's vectors start at the 16-byte boundary at or below its first element; this CTA holds [v0, v1).
         const int off = (int)(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(T)), V = (int)a.vocab;
         const int nvec = (off + V + VE - 1) / VE;
-        const int v0 = (int)((int64_t)nvec * rank / cluster), v1 = (int)((int64_t)nvec * (rank + 1) / cluster);
-        const int j0 = max(v0 * VE - off, 0), j1 = min(v1 * VE - off, V);     // its elements
+        const int v0 = (nvec * rank) >> log_cluster, v1 = (nvec * (rank + 1)) >> log_cluster, nv = v1 - v0;
+        const int e0 = v0 * VE - off;                                         // the entry in the slice's first element
+        const int j0 = max(e0, 0), j1 = min(v1 * VE - off, V);                // its entries
+        const int whole0 = e0 < 0 ? 1 : 0, whole1 = v1 * VE - off > V ? nv - 1 : nv;   // vectors that lie in the row entirely
         if (w == 0.0f) {
             if (rank == 0 && tid == 0) a.loss[t] = 0.0f;
             if constexpr (GRAD) for (int j = j0 + tid; j < j1; j += THREADS) g[j] = from_f32<T>(0.0f);
             continue;
         }
-        for (int v = v0 + tid; v < v1; v += THREADS) {
-            const int j = v * VE - off;
-            if (j >= 0 && j + VE <= V) {
-                copy16(vec + (v - v0), z + j);
-            } else {
+        {
+            const uint4* const src = reinterpret_cast<const uint4*>(z + e0);
+            for (int v = tid; v < nv; v += THREADS) {
+                if (v >= whole0 && v < whole1) {
+                    copy16(vec + v, src + v);
+                } else {
 #pragma unroll
-                for (int i = 0; i < VE; ++i)
-                    elem[(v - v0) * VE + i] = j + i >= 0 && j + i < V ? reinterpret_cast<const Bits*>(z)[j + i] : Row<T>::minus_inf;
+                    for (int i = 0; i < VE; ++i) {
+                        const int j = e0 + v * VE + i;
+                        elem[v * VE + i] = j >= 0 && j < V ? reinterpret_cast<const Bits*>(z)[j] : Row<T>::minus_inf;
+                    }
+                }
             }
         }
-        // Meanwhile one warp takes the teacher's entries.
+        // Meanwhile warp 0 takes the teacher's entries.
+        float s_t = 0.0f;
         if (warp == 0) {
-            float tmax = -INFINITY, st = 0.0f;
+            float tmax = -INFINITY;
             for (int k = lane; k < K; k += 32) {
                 const int64_t id = a.ids64 ? static_cast<const int64_t*>(a.ids)[t * K + k] : static_cast<const int32_t*>(a.ids)[t * K + k];
                 const bool ok = id >= 0 && id < V;
                 const float tl = ok ? load_f32(a.top_logits, a.top_dtype, t * K + k) : -INFINITY;
-                ids[k] = ok ? (int)id : -1;
+                slot[k] = ok && id >= j0 && id < j1 ? (int)id - e0 : -1;
                 lq[k] = tl;
                 tmax = fmaxf(tmax, tl);
             }
@@ -167,51 +184,38 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
                 // -infinity stays: its products with the two parts of 1 / tau could cancel to NaN
                 const float l = tl == -INFINITY ? tl : tail ? __fmaf_rn(tl, a.inv_tau, __fmaf_rn(tl, a.inv_tau_lo, -lse)) : (tl - tmax) * a.inv_tau;
                 lq[k] = l;
-                st += expf(l);
+                s_t += expf(l);
             }
-            st = warp_sum(st);
-            if (lane == 0) {
-                teacher[0] = st;
-                teacher[1] = tail || !(st > 0.0f) ? 0.0f : logf(st);
+            s_t = warp_sum(s_t);
+            if (!tail && s_t > 0.0f) {
+                const float log_t = logf(s_t);
+                for (int k = lane; k < K; k += 32) lq[k] -= log_t;
             }
         }
         copies_landed();
         __syncthreads();
-        const float s_t = teacher[0], log_t = teacher[1];
         // The listed entries of this slice leave it. An entry first puts its number into its element: where it then finds
         // another one, an id is listed twice.
         int twice = 0;
-        for (int k = tid; k < K; k += THREADS) {
-            const int id = ids[k], e = id + off - v0 * VE;
-            if (id >= j0 && id < j1) zk[k] = to_f32(reinterpret_cast<const T*>(elem)[e]);
-        }
-        __syncthreads();
-        for (int k = tid; k < K; k += THREADS) {
-            const int id = ids[k];
-            if (id >= j0 && id < j1) elem[id + off - v0 * VE] = (Bits)k;
-        }
-        __syncthreads();
-        for (int k = tid; k < K; k += THREADS) {
-            const int id = ids[k];
-            if (id >= j0 && id < j1) twice |= elem[id + off - v0 * VE] != (Bits)k;
-        }
-        twice = __syncthreads_or(twice);
-        float m_top = -INFINITY, s_top = 0.0f, n_top = 0.0f;
-        for (int k = tid; k < K; k += THREADS) {
-            const int id = ids[k];
-            if (id >= j0 && id < j1) {
-                elem[id + off - v0 * VE] = Row<T>::minus_inf;
-                m_top = fmaxf(m_top, zk[k]);
+        if (entries) {
+            const auto together = [&] { asm volatile("bar.sync 1, %0;" ::"r"(estride) : "memory"); };
+            float m_top = -INFINITY, s_top = 0.0f, n_top = 0.0f;
+            for (int k = tid; k < K; k += estride) {
+                const int e = slot[k];
+                if (e >= 0) m_top = fmaxf(m_top, zk[k] = to_f32(reinterpret_cast<const T*>(elem)[e]));
             }
-        }
-        __syncthreads();
-        if (warp * 32 < K) {
             m_top = warp_max1(m_top);
-            for (int k = tid; k < K; k += THREADS) {
-                const int id = ids[k];
-                if (id < j0 || id >= j1) continue;
+            together();
+            for (int k = tid; k < K; k += estride) if (const int e = slot[k]; e >= 0) elem[e] = (Bits)k;
+            together();
+            for (int k = tid; k < K; k += estride) if (const int e = slot[k]; e >= 0) twice |= elem[e] != (Bits)k;
+            asm volatile("{\n.reg .pred p, q;\nsetp.ne.s32 p, %1, 0;\nbar.red.or.pred q, 1, %2, p;\nselp.s32 %0, 1, 0, q;\n}" : "=r"(twice) : "r"(twice), "r"(estride) : "memory");
+            for (int k = tid; k < K; k += estride) {
+                const int e = slot[k];
+                if (e < 0) continue;
+                elem[e] = Row<T>::minus_inf;
                 bool first = true;       // every id counts once
-                if (twice) for (int i = 0; i < k; ++i) first &= ids[i] != id;
+                if (twice) for (int i = 0; i < k; ++i) first &= slot[i] != e;
                 if (first) {
                     s_top += ex2((zk[k] - finite_ref(m_top)) * c);
                     n_top += 1.0f;
@@ -219,17 +223,18 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
             }
             s_top = warp_sum(s_top);
             n_top = warp_sum(n_top);
+            if (lane == 0) { part[warp][P_MTOP] = m_top; part[warp][P_STOP] = s_top; part[warp][P_NTOP] = n_top; }
         }
-        VecMax<T> vm;
-#pragma unroll 4
-        for (int v = tid; v < v1 - v0; v += THREADS) vm.add(vec[v]);
-        float m_rest = warp_max1(vm.value()), s_rest = 0.0f;
+        __syncthreads();
         {
-            const float ref = finite_ref(m_rest);
-            const float2 neg = splat(-ref), c2 = splat(c);
+            VecMax<T> vm;
+#pragma unroll 4
+            for (int v = tid; v < nv; v += THREADS) vm.add(vec[v]);
+            const float m = warp_max1(vm.value());
+            const float2 neg = splat(-finite_ref(m)), c2 = splat(c);
             float2 sum = splat(0.0f);
 #pragma unroll 2
-            for (int v = tid; v < v1 - v0; v += THREADS) {
+            for (int v = tid; v < nv; v += THREADS) {
                 float2 x[VE / 2];
                 to_pairs<T>(vec[v], x);
 #pragma unroll
@@ -238,61 +243,81 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
                     sum = add2_rn(sum, make_float2(ex2(y.x), ex2(y.y)));
                 }
             }
-            s_rest = warp_sum(sum.x + sum.y);
-        }
-        if (lane == 0) {
-            part[warp][P_MREST] = m_rest; part[warp][P_SREST] = s_rest;
-            part[warp][P_MTOP] = m_top; part[warp][P_STOP] = s_top; part[warp][P_NTOP] = n_top;
+            const float s = warp_sum(sum.x + sum.y);
+            if (lane == 0) { part[warp][P_MREST] = m; part[warp][P_SREST] = s; }
         }
         __syncthreads();
-        {
-            const bool in = lane < WARPS;
-            float2 r = join_lanes(in ? part[lane][P_MREST] : -INFINITY, in ? part[lane][P_SREST] : 0.0f, c);
-            m_rest = r.x; s_rest = r.y;
-            r = join_lanes(in ? part[lane][P_MTOP] : -INFINITY, in ? part[lane][P_STOP] : 0.0f, c);
-            m_top = r.x; s_top = r.y;
-            n_top = warp_sum(in ? part[lane][P_NTOP] : 0.0f);
-        }
-        if (cluster > 1) {
-            if (tid < cluster) {
-                float* const mine = ranks[rank];
-                store_at(mine + P_MREST, tid, m_rest); store_at(mine + P_SREST, tid, s_rest);
-                store_at(mine + P_MTOP, tid, m_top); store_at(mine + P_STOP, tid, s_top); store_at(mine + P_NTOP, tid, n_top);
+        float m = 0.0f, m_rest = 0.0f, s_rest = 0.0f, log_s = 0.0f, s = 0.0f, q_rest = 0.0f;
+        if (warp == 0) {
+            bool in = lane < WARPS;
+            float2 rest = join_lanes(in ? part[lane][P_MREST] : -INFINITY, in ? part[lane][P_SREST] : 0.0f, c);
+            in = lane < entry_warps;
+            float2 top = join_lanes(in ? part[lane][P_MTOP] : -INFINITY, in ? part[lane][P_STOP] : 0.0f, c);
+            float n_top = warp_sum(in ? part[lane][P_NTOP] : 0.0f);
+            if (log_cluster) {
+                if (lane < cluster) {
+                    float* const mine = ranks[rank];
+                    store_at(mine + P_MREST, lane, rest.x); store_at(mine + P_SREST, lane, rest.y);
+                    store_at(mine + P_MTOP, lane, top.x); store_at(mine + P_STOP, lane, top.y); store_at(mine + P_NTOP, lane, n_top);
+                }
             }
-            cluster_barrier();
-            const bool in = lane < cluster;
-            const float* const theirs = ranks[in ? lane : 0];
-            float2 r = join_lanes(in ? theirs[P_MREST] : -INFINITY, in ? theirs[P_SREST] : 0.0f, c);
-            m_rest = r.x; s_rest = r.y;
-            r = join_lanes(in ? theirs[P_MTOP] : -INFINITY, in ? theirs[P_STOP] : 0.0f, c);
-            m_top = r.x; s_top = r.y;
-            n_top = warp_sum(in ? theirs[P_NTOP] : 0.0f);
+            part[0][P_MREST] = rest.x; part[0][P_SREST] = rest.y; part[0][P_MTOP] = top.x; part[0][P_STOP] = top.y; part[0][P_NTOP] = n_top;
         }
-        const float m = finite_ref(fmaxf(m_rest, m_top));
-        const float f_rest = ex2((m_rest - m) * c);                    // 0 when nothing is left out
-        const float s = __fmaf_rn(s_rest, f_rest, s_top * ex2((m_top - m) * c));
-        const float log_s = logf(s), inv_s = s > 0.0f || s != s ? 1.0f / s : 0.0f;
-        const float q_rest = tail && n_top < (float)V ? fmaxf(1.0f - s_t, 0.0f) : 0.0f;
-        const float Q = tail ? s_t + q_rest : (s_t > 0.0f || s_t != s_t) ? 1.0f : 0.0f;
-        const float scale = w * a.inv_tau;
-        if (warp * 32 < K) {
+        if (log_cluster) cluster_barrier();
+        if (warp == 0) {
+            float2 rest, top;
+            float n_top;
+            if (log_cluster) {
+                const bool in = lane < cluster;
+                const float* const r = ranks[in ? lane : 0];
+                rest = join_lanes(in ? r[P_MREST] : -INFINITY, in ? r[P_SREST] : 0.0f, c);
+                top = join_lanes(in ? r[P_MTOP] : -INFINITY, in ? r[P_STOP] : 0.0f, c);
+                n_top = warp_sum(in ? r[P_NTOP] : 0.0f);
+            } else {
+                __syncwarp();
+                rest = make_float2(part[0][P_MREST], part[0][P_SREST]);
+                top = make_float2(part[0][P_MTOP], part[0][P_STOP]);
+                n_top = part[0][P_NTOP];
+            }
+            m_rest = rest.x; s_rest = rest.y;
+            m = finite_ref(fmaxf(m_rest, top.x));
+            const float f_rest = ex2((m_rest - m) * c);                    // 0 when nothing is left out
+            s = __fmaf_rn(s_rest, f_rest, top.y * ex2((top.x - m) * c));
+            const float inv_s = s > 0.0f || s != s ? 1.0f / s : 0.0f;
+            log_s = logf(s);
+            q_rest = tail && n_top < (float)V ? fmaxf(1.0f - s_t, 0.0f) : 0.0f;
+            const float Q = tail ? s_t + q_rest : (s_t > 0.0f || s_t != s_t) ? 1.0f : 0.0f;
+            const float scale = w * a.inv_tau;
+            // Left out: p_j (Q - q_rest / p_rest) with p_j = 2^(c (z_j - m_rest)) f_rest / s and p_rest = s_rest f_rest / s.
+            if (lane == 0) {
+                result.ref = finite_ref(m_rest);
+                result.coef = (Q * f_rest * inv_s - (s_rest > 0.0f ? q_rest / s_rest : 0.0f)) * scale;
+                result.m = m;
+                result.q_scale = Q * inv_s * scale;
+                result.scale = scale;
+                top_part[0][0] = log_s;
+                top_part[0][1] = s;
+            }
+        }
+        __syncthreads();
+        const RowResult res = result;
+        if (entries) {      // this slice's share of the loss
+            const float log_all = top_part[0][0], all = top_part[0][1];
             float l = 0.0f;
-            for (int k = tid; k < K; k += THREADS) {
-                const int id = ids[k];
-                if (id < j0 || id >= j1) continue;
-                const float lqk = lq[k] - log_t, q = expf(lqk);
-                if (q != 0.0f) l += q * (lqk - (zk[k] == -INFINITY && s == s ? -INFINITY : (zk[k] - m) * a.inv_tau - log_s));
+            for (int k = tid; k < K; k += estride) {
+                if (slot[k] < 0) continue;
+                const float q = expf(lq[k]);
+                if (q != 0.0f) l += q * (lq[k] - (zk[k] == -INFINITY && all == all ? -INFINITY : (zk[k] - res.m) * a.inv_tau - log_all));
             }
             l = warp_sum(l);
-            if (lane == 0) loss_part[warp] = l;
+            if (lane == 0) part[warp][P_MTOP] = l;
         }
         if constexpr (GRAD) {
-            // Left out: p_j (Q - q_rest / p_rest) with p_j = 2^(c (z_j - m_rest)) f_rest / s and p_rest = s_rest f_rest / s.
-            const float coef = (Q * f_rest * inv_s - (s_rest > 0.0f ? q_rest / s_rest : 0.0f)) * scale;
-            const float2 neg = splat(-finite_ref(m_rest)), c2 = splat(c), coef2 = splat(coef);
+            const float2 neg = splat(-res.ref), c2 = splat(c), coef2 = splat(res.coef);
             if ((reinterpret_cast<uintptr_t>(g) - reinterpret_cast<uintptr_t>(z)) % 16 == 0) {
-#pragma unroll 1
-                for (int v = tid; v < v1 - v0; v += THREADS) {
+                uint4* const dst = reinterpret_cast<uint4*>(g + e0);
+#pragma unroll 2
+                for (int v = tid; v < nv; v += THREADS) {
                     float2 x[VE / 2];
                     to_pairs<T>(vec[v], x);
 #pragma unroll
@@ -300,13 +325,14 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
                         const float2 y = mul2_rn(add2_rn(x[i], neg), c2);
                         x[i] = mul2_rn(make_float2(ex2(y.x), ex2(y.y)), coef2);
                     }
-                    const int j = (v0 + v) * VE - off;
-                    if (j >= 0 && j + VE <= V) {
-                        *reinterpret_cast<uint4*>(g + j) = from_pairs<T>(x);
+                    if (v >= whole0 && v < whole1) {
+                        dst[v] = from_pairs<T>(x);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < VE; ++i)
-                            if (j + i >= 0 && j + i < V) g[j + i] = from_f32<T>(i & 1 ? x[i / 2].y : x[i / 2].x);
+                        for (int i = 0; i < VE; ++i) {
+                            const int j = e0 + v * VE + i;
+                            if (j >= 0 && j < V) g[j] = from_f32<T>(i & 1 ? x[i / 2].y : x[i / 2].x);
+                        }
                     }
                 }
             } else {
@@ -319,8 +345,8 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
                     float2 x[VE / 2];
 #pragma unroll
                     for (int i = 0; i < VE; ++i) {
-                        const float zi = j + i >= j0 && j + i < j1 ? to_f32(reinterpret_cast<const T*>(elem)[j + i + off - v0 * VE]) : -INFINITY;
-                        (i & 1 ? x[i / 2].y : x[i / 2].x) = ex2((zi + neg.x) * c) * coef;
+                        const float zi = j + i >= j0 && j + i < j1 ? to_f32(reinterpret_cast<const T*>(elem)[j + i - e0]) : -INFINITY;
+                        (i & 1 ? x[i / 2].y : x[i / 2].x) = ex2((zi + neg.x) * c) * res.coef;
                     }
                     if (j >= j0 && j + VE <= j1) {
                         *reinterpret_cast<uint4*>(g + j) = from_pairs<T>(x);
@@ -334,34 +360,35 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
         }
         __syncthreads();        // the listed entries' gradients go over the slice's, and the warps' shares of the loss are there
         if constexpr (GRAD) {
-            for (int k = tid; k < K; k += THREADS) {
-                const int id = ids[k];
-                if (id < j0 || id >= j1) continue;
-                float q = 0.0f;
-                if (twice) {
-                    for (int i = 0; i < K; ++i) if (ids[i] == id) q += expf(lq[i] - log_t);
-                } else {
-                    q = expf(lq[k] - log_t);
+            if (entries) {
+                for (int k = tid; k < K; k += estride) {
+                    const int e = slot[k];
+                    if (e < 0) continue;
+                    float q = 0.0f;
+                    if (twice) {
+                        for (int i = 0; i < K; ++i) if (slot[i] == e) q += expf(lq[i]);
+                    } else {
+                        q = expf(lq[k]);
+                    }
+                    g[e0 + e] = from_f32<T>(__fmaf_rn(ex2((zk[k] - res.m) * c), res.q_scale, -q * res.scale));
                 }
-                g[id] = from_f32<T>((ex2((zk[k] - m) * c) * inv_s * Q - q) * scale);
             }
         }
         if (warp == 0) {
-            float l = warp_sum(lane < WARPS && lane * 32 < K ? loss_part[lane] : 0.0f);
-            if (cluster > 1) {
-                if (lane == 0) store_at(&loss_ranks[rank], 0, l);
-            } else if (lane == 0) {
-                if (q_rest > 0.0f) l += q_rest * (logf(q_rest) - (s_rest > 0.0f ? (m_rest - m) * a.inv_tau + logf(s_rest) - log_s : -INFINITY));
-                a.loss[t] = w * l;
+            float l = warp_sum(lane < entry_warps ? part[lane][P_MTOP] : 0.0f);
+            if (log_cluster) {
+                if (lane == 0) store_at(&ranks[rank][P_COUNT], 0, l);
             }
+            if (rank == 0 && q_rest > 0.0f) s_t = q_rest * (logf(q_rest) - (s_rest > 0.0f ? (m_rest - m) * a.inv_tau + logf(s_rest) - log_s : -INFINITY));
+            else s_t = 0.0f;
+            if (!log_cluster && lane == 0) a.loss[t] = w * (l + s_t);
         }
-        if (cluster > 1) {
+        if (log_cluster) {
             cluster_barrier();
             if (rank == 0 && tid == 0) {
                 float l = 0.0f;
-                for (int r = 0; r < cluster; ++r) l += loss_ranks[r];
-                if (q_rest > 0.0f) l += q_rest * (logf(q_rest) - (s_rest > 0.0f ? (m_rest - m) * a.inv_tau + logf(s_rest) - log_s : -INFINITY));
-                a.loss[t] = w * l;
+                for (int r = 0; r < cluster; ++r) l += ranks[r][P_COUNT];
+                a.loss[t] = w * (l + s_t);
             }
         } else {
             __syncthreads();
@@ -370,7 +397,8 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
 }
 
 template <typename T, int THREADS, bool GRAD>
-cudaError_t launch(const DistillArgs& a, int cluster, int slice_vecs, size_t bytes, cudaStream_t s) {
+cudaError_t launch(const DistillArgs& a, int log_cluster, int slice_vecs, size_t bytes, cudaStream_t s) {
+    const int cluster = 1 << log_cluster;
     auto kernel = distill_kernel<T, THREADS, GRAD>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != cudaSuccess) return e;
@@ -386,7 +414,7 @@ cudaError_t launch(const DistillArgs& a, int cluster, int slice_vecs, size_t byt
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = cluster > 1 ? 1 : 0;
-    e = cudaLaunchKernelEx(&cfg, kernel, a, cluster, slice_vecs);
+    e = cudaLaunchKernelEx(&cfg, kernel, a, log_cluster, slice_vecs, std::min(THREADS / 32, (a.top + 63) / 64));
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -397,15 +425,15 @@ cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, cudaStream_t 
     const int64_t row_vecs = a.vocab * es / 16 + 2;    // however the row is aligned
     // Slices of up to 64 KB, three of which an SM holds at a time; eight CTAs at most. Few rows are split further, until every
     // SM has a CTA or a slice is down to 8 KB.
-    int cluster = 1;
-    while (cluster < kMaxCluster && row_vecs > cluster * (int64_t)4096) cluster *= 2;
-    while (cluster < kMaxCluster && a.tokens * cluster < 148 && row_vecs > cluster * (int64_t)1024) cluster *= 2;
-    const int slice = (int)((row_vecs + cluster - 1) / cluster) + 1;
+    int log_cluster = 0;
+    while (log_cluster < 3 && row_vecs > (int64_t)4096 << log_cluster) ++log_cluster;
+    while (log_cluster < 3 && a.tokens << log_cluster < 148 && row_vecs > (int64_t)1024 << log_cluster) ++log_cluster;
+    const int slice = (int)((row_vecs + (1 << log_cluster) - 1) >> log_cluster) + 1;
     const size_t bytes = (size_t)slice * 16 + (size_t)a.top * 12;
     return with_dtype(logits_dtype, [&](auto t) {
         using T = decltype(t);
-        if (slice <= 1024) return a.grad ? launch<T, 128, true>(a, cluster, slice, bytes, s) : launch<T, 128, false>(a, cluster, slice, bytes, s);
-        return a.grad ? launch<T, 512, true>(a, cluster, slice, bytes, s) : launch<T, 512, false>(a, cluster, slice, bytes, s);
+        if (slice <= 1024) return a.grad ? launch<T, 128, true>(a, log_cluster, slice, bytes, s) : launch<T, 128, false>(a, log_cluster, slice, bytes, s);
+        return a.grad ? launch<T, 256, true>(a, log_cluster, slice, bytes, s) : launch<T, 256, false>(a, log_cluster, slice, bytes, s);
     });
 }
 
