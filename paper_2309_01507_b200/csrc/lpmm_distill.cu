@@ -20,6 +20,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxCluster = 8;
+constexpr int blocks_per_sm(int threads) { return threads == 256 ? 3 : 8; }
 
 __device__ __forceinline__ float ex2(float x) {
     float r;
@@ -45,9 +46,9 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void cluster_barrier() {
-    asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_barrier() { cluster_arrive(); cluster_wait(); }
 // Stores v at `here`'s place in the shared memory of CTA `rank` of the cluster.
 __device__ __forceinline__ void store_at(float* here, uint32_t rank, float v) {
     uint32_t there;
@@ -106,79 +107,99 @@ __device__ __forceinline__ float2 join_lanes(float m, float s, float c) {
 
 enum { P_MREST, P_SREST, P_MTOP, P_STOP, P_NTOP, P_COUNT };   // what warps, and then CTAs of a cluster, exchange
 
-// What one warp works out for a row and all others read.
-struct RowResult {
-    float ref, coef;           // left out: gradient = coef 2^(c (z - ref))
-    float m, q_scale, scale;   // listed: q_scale 2^(c (z - m)) - q scale
+// Where a CTA's slice of a row lies: whole 16-byte vectors from the boundary at or below the row's first element on.
+template <typename T> struct Slice {
+    const T* z;
+    int nv, e0, j0, j1;       // vectors; the row's entry in the first element; the entries [j0, j1) that lie in the row
+    int whole0, whole1;       // the vectors that do entirely
+    __device__ __forceinline__ Slice(const DistillArgs& a, int64_t t, int rank, int log_cluster) {
+        constexpr int VE = Row<T>::n;
+        z = static_cast<const T*>(a.logits) + t * a.logits_stride;
+        const int off = (int)(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(T)), V = (int)a.vocab;
+        const int n = (off + V + VE - 1) / VE, v0 = (n * rank) >> log_cluster, v1 = (n * (rank + 1)) >> log_cluster;
+        nv = v1 - v0;
+        e0 = v0 * VE - off;
+        j0 = max(e0, 0);
+        j1 = min(v1 * VE - off, V);
+        whole0 = e0 < 0 ? 1 : 0;
+        whole1 = v1 * VE - off > V ? nv - 1 : nv;
+    }
+    // Starts the copy of vector v; -infinity where it reaches out of the row.
+    __device__ __forceinline__ void fetch(uint4* vec, int v, int V) const {
+        if (v >= whole0 && v < whole1) {
+            copy16(vec + v, reinterpret_cast<const uint4*>(z + e0) + v);
+        } else {
+            using Bits = typename Row<T>::Bits;
+#pragma unroll
+            for (int i = 0; i < Row<T>::n; ++i) {
+                const int j = e0 + v * Row<T>::n + i;
+                reinterpret_cast<Bits*>(vec + v)[i] = j >= 0 && j < V ? reinterpret_cast<const Bits*>(z)[j] : Row<T>::minus_inf;
+            }
+        }
+    }
 };
 
-// One cluster of CTAs per row of logits, each CTA a slice of whole 16-byte vectors of it, which it holds in shared memory: the
-// row is read from HBM once, and the gradient written once. Every thread copies, reduces and writes the same vectors, so that
-// only the listed entries, which are taken out of the slice (set to -infinity), need barriers. The first `entry_warps` warps
-// take the listed entries, warp 0 the teacher and what is worked out once per row.
+// The first row from t on, in steps of `step`, that has a weight. weight_at() is asked 32 rows ahead, one per lane.
+__device__ __forceinline__ float weight_ahead(const DistillArgs& a, int64_t t, int64_t step) {
+    const int64_t i = t + (threadIdx.x & 31) * step;
+    return i < a.tokens && a.weights ? a.weights[i] : 1.0f;
+}
+__device__ __forceinline__ int64_t live_row(const DistillArgs& a, int64_t t, int64_t step, float ahead) {
+    for (;;) {
+        const uint32_t live = __ballot_sync(0xffffffffu, ahead != 0.0f);
+        if (live) return min(t + (__ffs(live) - 1) * step, a.tokens);
+        t += 32 * step;
+        ahead = weight_ahead(a, t, step);
+    }
+}
+
+// Barriers: all warps of the CTA, when a row and its teacher's side are in shared memory; the workers alone, within a row.
+template <int THREADS> __device__ __forceinline__ void row_ready() { asm volatile("bar.sync 0, %0;" ::"n"(THREADS + 32) : "memory"); }
+template <int THREADS> __device__ __forceinline__ void workers_together() { asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory"); }
+
+// One cluster of CTAs per row of logits, each CTA a slice of it, which it holds in shared memory: the row is read from HBM once,
+// and the gradient written once. Each of the THREADS workers copies, reduces and writes the same vectors of every row, so that
+// only the listed entries, which are taken out of the slice (set to -infinity), need barriers, and a worker fetches a vector
+// of the next row as soon as it is done with this row's. The first `entry_warps` warps take the listed entries; one more warp
+// prepares the teacher's side of the next row meanwhile.
 template <typename T, int THREADS, bool GRAD>
-__global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const DistillArgs a, const int log_cluster, const int slice_vecs, const int entry_warps) {
+__global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_kernel(const DistillArgs a, const int log_cluster, const int slice_vecs, const int entry_warps) {
     using Bits = typename Row<T>::Bits;
     constexpr int VE = Row<T>::n, WARPS = THREADS / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     uint4* const vec = reinterpret_cast<uint4*>(smem);
     Bits* const elem = reinterpret_cast<Bits*>(smem);
-    int* const slot = reinterpret_cast<int*>(vec + slice_vecs);   // K ids, later the element in the slice; -1: no entry here
-    float* const lq = reinterpret_cast<float*>(slot + a.top);     // logarithms of the teacher's probabilities
-    float* const zk = lq + a.top;                                 // the student's logits at the ids of this slice
-    __shared__ float part[WARPS][P_COUNT], top_part[WARPS][2];
-    __shared__ float ranks[kMaxCluster][P_COUNT + 2];
-    __shared__ RowResult result;
-    const int K = a.top, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, estride = entry_warps * 32;
+    const int K = a.top;
+    int* const slots = reinterpret_cast<int*>(vec + slice_vecs);   // 2 x K: the element in the slice; -1: no entry here
+    float* const lqs = reinterpret_cast<float*>(slots + 2 * K);    // 2 x K: logarithms of the teacher's probabilities
+    float* const zk = lqs + 2 * K;                                 // the student's logits at the slots
+    __shared__ float part[WARPS][P_COUNT], loss_part[WARPS], teacher[2][2];
+    __shared__ float ranks[kMaxCluster][P_COUNT + 1];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, estride = entry_warps * 32, V = (int)a.vocab;
     const int cluster = 1 << log_cluster, rank = log_cluster ? (int)cluster_rank() : 0;
     const float c = a.inv_tau * kLog2e;
     const bool tail = a.teacher_lse != nullptr, entries = warp < entry_warps;
+    const int64_t step = gridDim.x >> log_cluster, first_row = blockIdx.x >> log_cluster;
     if (log_cluster) cluster_barrier();       // every CTA is there before another stores into its shared memory
+    int64_t t = live_row(a, first_row, step, weight_ahead(a, first_row, step));
+    int buf = 0;
 
-    for (int64_t t = blockIdx.x >> log_cluster; t < a.tokens; t += gridDim.x >> log_cluster) {
-        const float w = a.weights ? a.weights[t] : 1.0f;
-        const T* const z = static_cast<const T*>(a.logits) + t * a.logits_stride;
-        T* const g = GRAD ? static_cast<T*>(a.grad) + t * a.grad_stride : nullptr;
-        // The row's vectors start at the 16-byte boundary at or below its first element; this CTA holds [v0, v1).
-        const int off = (int)(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(T)), V = (int)a.vocab;
-        const int nvec = (off + V + VE - 1) / VE;
-        const int v0 = (nvec * rank) >> log_cluster, v1 = (nvec * (rank + 1)) >> log_cluster, nv = v1 - v0;
-        const int e0 = v0 * VE - off;                                         // the entry in the slice's first element
-        const int j0 = max(e0, 0), j1 = min(v1 * VE - off, V);                // its entries
-        const int whole0 = e0 < 0 ? 1 : 0, whole1 = v1 * VE - off > V ? nv - 1 : nv;   // vectors that lie in the row entirely
-        if (w == 0.0f) {
-            if (rank == 0 && tid == 0) a.loss[t] = 0.0f;
-            if constexpr (GRAD) for (int j = j0 + tid; j < j1; j += THREADS) g[j] = from_f32<T>(0.0f);
-            continue;
-        }
-        {
-            const uint4* const src = reinterpret_cast<const uint4*>(z + e0);
-            for (int v = tid; v < nv; v += THREADS) {
-                if (v >= whole0 && v < whole1) {
-                    copy16(vec + v, src + v);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < VE; ++i) {
-                        const int j = e0 + v * VE + i;
-                        elem[v * VE + i] = j >= 0 && j < V ? reinterpret_cast<const Bits*>(z)[j] : Row<T>::minus_inf;
-                    }
-                }
-            }
-        }
-        // Meanwhile warp 0 takes the teacher's entries.
-        float s_t = 0.0f;
-        if (warp == 0) {
-            float tmax = -INFINITY;
+    if (warp == WARPS) {                      // the teacher
+        const auto prepare = [&](int64_t t, int buf) {
+            int* const slot = slots + buf * K;
+            float* const lq = lqs + buf * K;
+            const float w = a.weights ? a.weights[t] : 1.0f, lse = tail ? a.teacher_lse[t] : 0.0f;
+            const Slice<T> sl(a, t, rank, log_cluster);
+            float tmax = -INFINITY, s_t = 0.0f;
             for (int k = lane; k < K; k += 32) {
                 const int64_t id = a.ids64 ? static_cast<const int64_t*>(a.ids)[t * K + k] : static_cast<const int32_t*>(a.ids)[t * K + k];
-                const bool ok = id >= 0 && id < V;
-                const float tl = ok ? load_f32(a.top_logits, a.top_dtype, t * K + k) : -INFINITY;
-                slot[k] = ok && id >= j0 && id < j1 ? (int)id - e0 : -1;
+                float tl = load_f32(a.top_logits, a.top_dtype, t * K + k);
+                if (id < 0 || id >= V) tl = -INFINITY;
+                slot[k] = id >= sl.j0 && id < sl.j1 ? (int)id - sl.e0 : -1;
                 lq[k] = tl;
                 tmax = fmaxf(tmax, tl);
             }
             tmax = finite_ref(warp_max1(tmax));
-            const float lse = tail ? a.teacher_lse[t] : 0.0f;
             for (int k = lane; k < K; k += 32) {
                 const float tl = lq[k];
                 // -infinity stays: its products with the two parts of 1 / tau could cancel to NaN
@@ -191,9 +212,49 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
                 const float log_t = logf(s_t);
                 for (int k = lane; k < K; k += 32) lq[k] -= log_t;
             }
+            if (lane == 0) { teacher[buf][0] = s_t; teacher[buf][1] = w; }
+        };
+        if (t < a.tokens) prepare(t, 0);
+        while (t < a.tokens) {
+            const float ahead = weight_ahead(a, t + step, step);
+            row_ready<THREADS>();
+            if (log_cluster) cluster_arrive();
+            t = live_row(a, t + step, step, ahead);
+            if (t < a.tokens) prepare(t, buf ^= 1);
+            if (log_cluster) { cluster_wait(); cluster_barrier(); }
         }
+        return;
+    }
+
+    if (t < a.tokens) {
+        const Slice<T> sl(a, t, rank, log_cluster);
+        for (int v = tid; v < sl.nv; v += THREADS) sl.fetch(vec, v, V);
+    }
+    if (a.weights) {                          // rows without a weight, while the first one arrives
+        for (int64_t r = first_row; r < a.tokens; r += step) {
+            if (a.weights[r] != 0.0f) continue;
+            if (rank == 0 && tid == 0) a.loss[r] = 0.0f;
+            if constexpr (GRAD) {
+                T* const g = static_cast<T*>(a.grad) + r * a.grad_stride;
+                const Slice<T> sl(a, r, rank, log_cluster);
+                const int j0 = min(sl.j1, sl.j0 + (int)((16 - reinterpret_cast<uintptr_t>(g + sl.j0) % 16) % 16 / sizeof(T)));
+                const int n = (sl.j1 - j0) / VE, j1 = j0 + n * VE;
+                if (tid < j0 - sl.j0) g[sl.j0 + tid] = from_f32<T>(0.0f);
+                if (tid < sl.j1 - j1) g[j1 + tid] = from_f32<T>(0.0f);
+                for (int v = tid; v < n; v += THREADS) reinterpret_cast<uint4*>(g + j0)[v] = make_uint4(0, 0, 0, 0);
+            }
+        }
+    }
+
+    for (; t < a.tokens; buf ^= 1) {
+        const int* const slot = slots + buf * K;
+        const float* const lq = lqs + buf * K;
+        const Slice<T> sl(a, t, rank, log_cluster);
+        const int nv = sl.nv;
+        const float ahead = weight_ahead(a, t + step, step);
         copies_landed();
-        __syncthreads();
+        row_ready<THREADS>();
+        const float s_t = teacher[buf][0], w = teacher[buf][1];
         // The listed entries of this slice leave it. An entry first puts its number into its element: where it then finds
         // another one, an id is listed twice.
         int twice = 0;
@@ -225,7 +286,10 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
             n_top = warp_sum(n_top);
             if (lane == 0) { part[warp][P_MTOP] = m_top; part[warp][P_STOP] = s_top; part[warp][P_NTOP] = n_top; }
         }
-        __syncthreads();
+        workers_together<THREADS>();
+        const int64_t t_next = live_row(a, t + step, step, ahead);
+        const Slice<T> next(a, min(t_next, a.tokens - 1), rank, log_cluster);
+        const int nv_next = t_next < a.tokens ? next.nv : 0;
         {
             VecMax<T> vm;
 #pragma unroll 4
@@ -243,80 +307,61 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
                     sum = add2_rn(sum, make_float2(ex2(y.x), ex2(y.y)));
                 }
             }
+            if constexpr (!GRAD) for (int v = tid; v < nv_next; v += THREADS) next.fetch(vec, v, V);
             const float s = warp_sum(sum.x + sum.y);
             if (lane == 0) { part[warp][P_MREST] = m; part[warp][P_SREST] = s; }
         }
-        __syncthreads();
-        float m = 0.0f, m_rest = 0.0f, s_rest = 0.0f, log_s = 0.0f, s = 0.0f, q_rest = 0.0f;
-        if (warp == 0) {
+        workers_together<THREADS>();
+        float2 rest, top;
+        float n_top;
+        {
             bool in = lane < WARPS;
-            float2 rest = join_lanes(in ? part[lane][P_MREST] : -INFINITY, in ? part[lane][P_SREST] : 0.0f, c);
+            rest = join_lanes(in ? part[lane][P_MREST] : -INFINITY, in ? part[lane][P_SREST] : 0.0f, c);
             in = lane < entry_warps;
-            float2 top = join_lanes(in ? part[lane][P_MTOP] : -INFINITY, in ? part[lane][P_STOP] : 0.0f, c);
-            float n_top = warp_sum(in ? part[lane][P_NTOP] : 0.0f);
-            if (log_cluster) {
-                if (lane < cluster) {
-                    float* const mine = ranks[rank];
-                    store_at(mine + P_MREST, lane, rest.x); store_at(mine + P_SREST, lane, rest.y);
-                    store_at(mine + P_MTOP, lane, top.x); store_at(mine + P_STOP, lane, top.y); store_at(mine + P_NTOP, lane, n_top);
-                }
-            }
-            part[0][P_MREST] = rest.x; part[0][P_SREST] = rest.y; part[0][P_MTOP] = top.x; part[0][P_STOP] = top.y; part[0][P_NTOP] = n_top;
+            top = join_lanes(in ? part[lane][P_MTOP] : -INFINITY, in ? part[lane][P_STOP] : 0.0f, c);
+            n_top = warp_sum(in ? part[lane][P_NTOP] : 0.0f);
         }
-        if (log_cluster) cluster_barrier();
-        if (warp == 0) {
-            float2 rest, top;
-            float n_top;
-            if (log_cluster) {
-                const bool in = lane < cluster;
-                const float* const r = ranks[in ? lane : 0];
-                rest = join_lanes(in ? r[P_MREST] : -INFINITY, in ? r[P_SREST] : 0.0f, c);
-                top = join_lanes(in ? r[P_MTOP] : -INFINITY, in ? r[P_STOP] : 0.0f, c);
-                n_top = warp_sum(in ? r[P_NTOP] : 0.0f);
-            } else {
-                __syncwarp();
-                rest = make_float2(part[0][P_MREST], part[0][P_SREST]);
-                top = make_float2(part[0][P_MTOP], part[0][P_STOP]);
-                n_top = part[0][P_NTOP];
+        if (log_cluster) {
+            if (tid < cluster) {
+                float* const mine = ranks[rank];
+                store_at(mine + P_MREST, tid, rest.x); store_at(mine + P_SREST, tid, rest.y);
+                store_at(mine + P_MTOP, tid, top.x); store_at(mine + P_STOP, tid, top.y); store_at(mine + P_NTOP, tid, n_top);
             }
-            m_rest = rest.x; s_rest = rest.y;
-            m = finite_ref(fmaxf(m_rest, top.x));
-            const float f_rest = ex2((m_rest - m) * c);                    // 0 when nothing is left out
-            s = __fmaf_rn(s_rest, f_rest, top.y * ex2((top.x - m) * c));
-            const float inv_s = s > 0.0f || s != s ? 1.0f / s : 0.0f;
-            log_s = logf(s);
-            q_rest = tail && n_top < (float)V ? fmaxf(1.0f - s_t, 0.0f) : 0.0f;
-            const float Q = tail ? s_t + q_rest : (s_t > 0.0f || s_t != s_t) ? 1.0f : 0.0f;
-            const float scale = w * a.inv_tau;
-            // Left out: p_j (Q - q_rest / p_rest) with p_j = 2^(c (z_j - m_rest)) f_rest / s and p_rest = s_rest f_rest / s.
-            if (lane == 0) {
-                result.ref = finite_ref(m_rest);
-                result.coef = (Q * f_rest * inv_s - (s_rest > 0.0f ? q_rest / s_rest : 0.0f)) * scale;
-                result.m = m;
-                result.q_scale = Q * inv_s * scale;
-                result.scale = scale;
-                top_part[0][0] = log_s;
-                top_part[0][1] = s;
-            }
+            cluster_barrier();
+            const bool in = lane < cluster;
+            const float* const r = ranks[in ? lane : 0];
+            rest = join_lanes(in ? r[P_MREST] : -INFINITY, in ? r[P_SREST] : 0.0f, c);
+            top = join_lanes(in ? r[P_MTOP] : -INFINITY, in ? r[P_STOP] : 0.0f, c);
+            n_top = warp_sum(in ? r[P_NTOP] : 0.0f);
         }
-        __syncthreads();
-        const RowResult res = result;
+        const float m_rest = rest.x, s_rest = rest.y, m = finite_ref(fmaxf(m_rest, top.x));
+        const float f_rest = ex2((m_rest - m) * c);                    // 0 when nothing is left out
+        const float s = __fmaf_rn(s_rest, f_rest, top.y * ex2((top.x - m) * c));
+        const float inv_s = s > 0.0f || s != s ? 1.0f / s : 0.0f;
+        const float q_rest = tail && n_top < (float)V ? fmaxf(1.0f - s_t, 0.0f) : 0.0f;
+        const float Q = tail ? s_t + q_rest : (s_t > 0.0f || s_t != s_t) ? 1.0f : 0.0f;
+        const float scale = w * a.inv_tau;
         if (entries) {      // this slice's share of the loss
-            const float log_all = top_part[0][0], all = top_part[0][1];
+            const float log_s = logf(s);
             float l = 0.0f;
             for (int k = tid; k < K; k += estride) {
                 if (slot[k] < 0) continue;
                 const float q = expf(lq[k]);
-                if (q != 0.0f) l += q * (lq[k] - (zk[k] == -INFINITY && all == all ? -INFINITY : (zk[k] - res.m) * a.inv_tau - log_all));
+                if (q != 0.0f) l += q * (lq[k] - (zk[k] == -INFINITY && s == s ? -INFINITY : (zk[k] - m) * a.inv_tau - log_s));
             }
             l = warp_sum(l);
-            if (lane == 0) part[warp][P_MTOP] = l;
+            if (tid == 0 && rank == 0 && q_rest > 0.0f)
+                l += q_rest * (logf(q_rest) - (s_rest > 0.0f ? (m_rest - m) * a.inv_tau + logf(s_rest) - log_s : -INFINITY));
+            if (lane == 0) loss_part[warp] = l;
         }
+        bool fetched = !GRAD;
+        T* const g = GRAD ? static_cast<T*>(a.grad) + t * a.grad_stride : nullptr;
         if constexpr (GRAD) {
-            const float2 neg = splat(-res.ref), c2 = splat(c), coef2 = splat(res.coef);
-            if ((reinterpret_cast<uintptr_t>(g) - reinterpret_cast<uintptr_t>(z)) % 16 == 0) {
-                uint4* const dst = reinterpret_cast<uint4*>(g + e0);
-#pragma unroll 2
+            // Left out: p_j (Q - q_rest / p_rest) with p_j = 2^(c (z_j - m_rest)) f_rest / s and p_rest = s_rest f_rest / s.
+            const float coef = (Q * f_rest * inv_s - (s_rest > 0.0f ? q_rest / s_rest : 0.0f)) * scale;
+            const float2 neg = splat(-finite_ref(m_rest)), c2 = splat(c), coef2 = splat(coef);
+            if ((reinterpret_cast<uintptr_t>(g) - reinterpret_cast<uintptr_t>(sl.z)) % 16 == 0) {
+                uint4* const dst = reinterpret_cast<uint4*>(g + sl.e0);
                 for (int v = tid; v < nv; v += THREADS) {
                     float2 x[VE / 2];
                     to_pairs<T>(vec[v], x);
@@ -325,42 +370,48 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
                         const float2 y = mul2_rn(add2_rn(x[i], neg), c2);
                         x[i] = mul2_rn(make_float2(ex2(y.x), ex2(y.y)), coef2);
                     }
-                    if (v >= whole0 && v < whole1) {
+                    if (v < nv_next) next.fetch(vec, v, V);
+                    if (v >= sl.whole0 && v < sl.whole1) {
                         dst[v] = from_pairs<T>(x);
                     } else {
 #pragma unroll
                         for (int i = 0; i < VE; ++i) {
-                            const int j = e0 + v * VE + i;
+                            const int j = sl.e0 + v * VE + i;
                             if (j >= 0 && j < V) g[j] = from_f32<T>(i & 1 ? x[i / 2].y : x[i / 2].x);
                         }
                     }
                 }
+                // the next row may have a vector more
+                for (int v = tid + (nv - tid + THREADS - 1) / THREADS * THREADS; v < nv_next; v += THREADS) next.fetch(vec, v, V);
+                fetched = true;
             } else {
                 // The gradient's rows are aligned otherwise than the logits': its own vectors, gathered element by element.
                 const int goff = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T));
-                const int u1 = (j1 + goff + VE - 1) / VE;
+                const int u1 = (sl.j1 + goff + VE - 1) / VE;
 #pragma unroll 1
-                for (int u = (j0 + goff) / VE + tid; u < u1; u += THREADS) {
+                for (int u = (sl.j0 + goff) / VE + tid; u < u1; u += THREADS) {
                     const int j = u * VE - goff;
                     float2 x[VE / 2];
 #pragma unroll
                     for (int i = 0; i < VE; ++i) {
-                        const float zi = j + i >= j0 && j + i < j1 ? to_f32(reinterpret_cast<const T*>(elem)[j + i - e0]) : -INFINITY;
-                        (i & 1 ? x[i / 2].y : x[i / 2].x) = ex2((zi + neg.x) * c) * res.coef;
+                        const float zi = j + i >= sl.j0 && j + i < sl.j1 ? to_f32(reinterpret_cast<const T*>(elem)[j + i - sl.e0]) : -INFINITY;
+                        (i & 1 ? x[i / 2].y : x[i / 2].x) = ex2((zi + neg.x) * c) * coef;
                     }
-                    if (j >= j0 && j + VE <= j1) {
+                    if (j >= sl.j0 && j + VE <= sl.j1) {
                         *reinterpret_cast<uint4*>(g + j) = from_pairs<T>(x);
                     } else {
 #pragma unroll
                         for (int i = 0; i < VE; ++i)
-                            if (j + i >= j0 && j + i < j1) g[j + i] = from_f32<T>(i & 1 ? x[i / 2].y : x[i / 2].x);
+                            if (j + i >= sl.j0 && j + i < sl.j1) g[j + i] = from_f32<T>(i & 1 ? x[i / 2].y : x[i / 2].x);
                     }
                 }
             }
         }
-        __syncthreads();        // the listed entries' gradients go over the slice's, and the warps' shares of the loss are there
+        workers_together<THREADS>();        // the listed entries' gradients go over the slice's, and the warps' shares of the loss are there
+        if (!fetched) for (int v = tid; v < nv_next; v += THREADS) next.fetch(vec, v, V);
         if constexpr (GRAD) {
             if (entries) {
+                const float q_scale = Q * inv_s * scale;
                 for (int k = tid; k < K; k += estride) {
                     const int e = slot[k];
                     if (e < 0) continue;
@@ -370,29 +421,26 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
                     } else {
                         q = expf(lq[k]);
                     }
-                    g[e0 + e] = from_f32<T>(__fmaf_rn(ex2((zk[k] - res.m) * c), res.q_scale, -q * res.scale));
+                    g[sl.e0 + e] = from_f32<T>(__fmaf_rn(ex2((zk[k] - m) * c), q_scale, -q * scale));
                 }
             }
         }
         if (warp == 0) {
-            float l = warp_sum(lane < entry_warps ? part[lane][P_MTOP] : 0.0f);
-            if (log_cluster) {
-                if (lane == 0) store_at(&ranks[rank][P_COUNT], 0, l);
+            const float l = warp_sum(lane < entry_warps ? loss_part[lane] : 0.0f);
+            if (lane == 0) {
+                if (log_cluster) store_at(&ranks[rank][P_COUNT], 0, l);
+                else a.loss[t] = w * l;
             }
-            if (rank == 0 && q_rest > 0.0f) s_t = q_rest * (logf(q_rest) - (s_rest > 0.0f ? (m_rest - m) * a.inv_tau + logf(s_rest) - log_s : -INFINITY));
-            else s_t = 0.0f;
-            if (!log_cluster && lane == 0) a.loss[t] = w * (l + s_t);
         }
         if (log_cluster) {
             cluster_barrier();
             if (rank == 0 && tid == 0) {
                 float l = 0.0f;
                 for (int r = 0; r < cluster; ++r) l += ranks[r][P_COUNT];
-                a.loss[t] = w * (l + s_t);
+                a.loss[t] = w * l;
             }
-        } else {
-            __syncthreads();
         }
+        t = t_next;
     }
 }
 
@@ -400,12 +448,14 @@ template <typename T, int THREADS, bool GRAD>
 cudaError_t launch(const DistillArgs& a, int log_cluster, int slice_vecs, size_t bytes, cudaStream_t s) {
     const int cluster = 1 << log_cluster;
     auto kernel = distill_kernel<T, THREADS, GRAD>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    cudaError_t e = bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) : cudaSuccess;
     if (e != cudaSuccess) return e;
-    const int64_t rows = a.tokens < (1 << 24) ? a.tokens : 1 << 24;
+    // As many CTAs as the SMs hold (their registers: see the launch bounds), each on every so manieth row.
+    const int per_sm = std::max(1, std::min(blocks_per_sm(THREADS), (int)(227 * 1024 / (bytes + 2048))));
+    const int64_t rows = std::min<int64_t>(a.tokens, (148 * per_sm) >> log_cluster);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * cluster));
-    cfg.blockDim = dim3(THREADS);
+    cfg.blockDim = dim3(THREADS + 32);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = s;
     cudaLaunchAttribute attr;
@@ -429,7 +479,7 @@ cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, cudaStream_t 
     while (log_cluster < 3 && row_vecs > (int64_t)4096 << log_cluster) ++log_cluster;
     while (log_cluster < 3 && a.tokens << log_cluster < 148 && row_vecs > (int64_t)1024 << log_cluster) ++log_cluster;
     const int slice = (int)((row_vecs + (1 << log_cluster) - 1) >> log_cluster) + 1;
-    const size_t bytes = (size_t)slice * 16 + (size_t)a.top * 12;
+    const size_t bytes = (size_t)slice * 16 + (size_t)a.top * 20;
     return with_dtype(logits_dtype, [&](auto t) {
         using T = decltype(t);
         if (slice <= 1024) return a.grad ? launch<T, 128, true>(a, log_cluster, slice, bytes, s) : launch<T, 128, false>(a, log_cluster, slice, bytes, s);
