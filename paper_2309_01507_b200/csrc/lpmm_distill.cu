@@ -32,9 +32,11 @@ __device__ __forceinline__ float warp_max1(float x) {   // one instruction on sm
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float warp_sum(float x) {
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    return x;
+// The sum over the first LANES lanes, in every lane.
+template <int LANES> __device__ __forceinline__ float sum_lanes(float x) {
+#pragma unroll
+    for (int d = LANES / 2; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    return LANES < 32 ? __shfl_sync(0xffffffffu, x, 0) : x;
 }
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(void* dst, const void* src) {
@@ -100,12 +102,10 @@ template <> struct VecMax<__half> : PairMax<__half2, __half> {};
 // A class of a row's entries (those left out, or the listed ones): the maximum of its logits and the sum of the powers relative
 // to it. Parts are joined by bringing them to the larger maximum; an empty part has maximum -infinity and sum 0.
 __device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.0f : m; }
-__device__ __forceinline__ float2 join_lanes(float m, float s, float c) {
+template <int LANES> __device__ __forceinline__ float2 join_lanes(float m, float s, float c) {
     const float M = warp_max1(m);
-    return make_float2(M, warp_sum(s * ex2((m - finite_ref(M)) * c)));
+    return make_float2(M, sum_lanes<LANES>(s * ex2((m - finite_ref(M)) * c)));
 }
-
-enum { P_MREST, P_SREST, P_MTOP, P_STOP, P_NTOP, P_COUNT };   // what warps, and then CTAs of a cluster, exchange
 
 // Where a CTA's slice of a row lies: whole 16-byte vectors from the boundary at or below the row's first element on.
 template <typename T> struct Slice {
@@ -153,75 +153,199 @@ __device__ __forceinline__ int64_t live_row(const DistillArgs& a, int64_t t, int
     }
 }
 
-// Barriers: all warps of the CTA, when a row and its teacher's side are in shared memory; the workers alone, within a row.
-template <int THREADS> __device__ __forceinline__ void row_ready() { asm volatile("bar.sync 0, %0;" ::"n"(THREADS + 32) : "memory"); }
-template <int THREADS> __device__ __forceinline__ void workers_together() { asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory"); }
+// Named barriers between the workers and the teacher's warp; "arrive" does not wait.
+enum { B_ROW = 1, B_TAKEN, B_PARTS, B_PARTS_SEEN, B_WRITTEN };
+template <int THREADS> __device__ __forceinline__ void meet(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(THREADS + 32) : "memory"); }
+template <int THREADS> __device__ __forceinline__ void pass(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(THREADS + 32) : "memory"); }
+
+// What the classes of a row come to.
+struct RowSums {
+    float m, m_rest, s_rest, f_rest, s, inv_s, q_rest, Q;
+    __device__ __forceinline__ RowSums(float2 rest, float2 top, float n_top, float s_t, float c, bool tail, int V) {
+        m_rest = rest.x; s_rest = rest.y;
+        m = finite_ref(fmaxf(rest.x, top.x));
+        f_rest = ex2((m_rest - m) * c);                    // 0 when nothing is left out
+        s = __fmaf_rn(s_rest, f_rest, top.y * ex2((top.x - m) * c));
+        inv_s = s > 0.0f || s != s ? 1.0f / s : 0.0f;
+        q_rest = tail && n_top < (float)V ? fmaxf(1.0f - s_t, 0.0f) : 0.0f;
+        Q = tail ? s_t + q_rest : (s_t > 0.0f || s_t != s_t) ? 1.0f : 0.0f;
+    }
+};
 
 // One cluster of CTAs per row of logits, each CTA a slice of it, which it holds in shared memory: the row is read from HBM once,
-// and the gradient written once. Each of the THREADS workers copies, reduces and writes the same vectors of every row, so that
-// only the listed entries, which are taken out of the slice (set to -infinity), need barriers, and a worker fetches a vector
-// of the next row as soon as it is done with this row's. The first `entry_warps` warps take the listed entries; one more warp
-// prepares the teacher's side of the next row meanwhile.
+// and the gradient written once. Each of the THREADS workers copies, reduces and writes the same vectors of every row and fetches
+// a vector of the next row as soon as it is done with this row's. One more warp, the teacher, has all that concerns the listed
+// entries: it prepares their q a row ahead, takes them out of the slice (sets them to -infinity), adds up the loss and writes
+// their gradients over the workers'.
 template <typename T, int THREADS, bool GRAD>
-__global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_kernel(const DistillArgs a, const int log_cluster, const int slice_vecs, const int entry_warps) {
-    using Bits = typename Row<T>::Bits;
+__global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_kernel(const DistillArgs a, const int log_cluster, const int slice_vecs) {
     constexpr int VE = Row<T>::n, WARPS = THREADS / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     uint4* const vec = reinterpret_cast<uint4*>(smem);
-    Bits* const elem = reinterpret_cast<Bits*>(smem);
+    T* const elem = reinterpret_cast<T*>(smem);
     const int K = a.top;
-    int* const slots = reinterpret_cast<int*>(vec + slice_vecs);   // 2 x K: the element in the slice; -1: no entry here
-    float* const lqs = reinterpret_cast<float*>(slots + 2 * K);    // 2 x K: logarithms of the teacher's probabilities
-    float* const zk = lqs + 2 * K;                                 // the student's logits at the slots
-    __shared__ float part[WARPS][P_COUNT], loss_part[WARPS], teacher[2][2];
-    __shared__ float ranks[kMaxCluster][P_COUNT + 1];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, estride = entry_warps * 32, V = (int)a.vocab;
+    int* const slots = reinterpret_cast<int*>(vec + slice_vecs);         // 2 x K: the entry's element in the slice; -1: not here
+    float* const lqs = reinterpret_cast<float*>(slots + 2 * K);          // 2 x K: logarithms of the teacher's probabilities
+    float* const zk = lqs + 2 * K;                                       // K: the student's logits
+    uint32_t* const bits = reinterpret_cast<uint32_t*>(zk + K);          // one per element, to find ids that are listed twice
+    __shared__ float part[WARPS][2], top_part[3], teacher[2];
+    __shared__ float ranks[2][kMaxCluster][5], loss_ranks[2][kMaxCluster];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, V = (int)a.vocab;
     const int cluster = 1 << log_cluster, rank = log_cluster ? (int)cluster_rank() : 0;
     const float c = a.inv_tau * kLog2e;
-    const bool tail = a.teacher_lse != nullptr, entries = warp < entry_warps;
+    const bool tail = a.teacher_lse != nullptr;
     const int64_t step = gridDim.x >> log_cluster, first_row = blockIdx.x >> log_cluster;
     if (log_cluster) cluster_barrier();       // every CTA is there before another stores into its shared memory
     int64_t t = live_row(a, first_row, step, weight_ahead(a, first_row, step));
-    int buf = 0;
+    int parity = 0;
+    // The row's classes over the whole cluster, from the ranks' parts.
+    const auto joined = [&](float2& rest, float2& top, float& n_top) {
+        const bool in = lane < cluster;
+        const float* const r = ranks[parity][in ? lane : 0];
+        rest = join_lanes<kMaxCluster>(in ? r[0] : -INFINITY, in ? r[1] : 0.0f, c);
+        top = join_lanes<kMaxCluster>(in ? r[2] : -INFINITY, in ? r[3] : 0.0f, c);
+        n_top = sum_lanes<kMaxCluster>(in ? r[4] : 0.0f);
+    };
+    // ... and over this CTA, from the warps' parts.
+    const auto own_classes = [&](float2& rest, float2& top, float& n_top) {
+        const bool in = lane < WARPS;
+        rest = join_lanes<WARPS>(in ? part[lane][0] : -INFINITY, in ? part[lane][1] : 0.0f, c);
+        top = make_float2(top_part[0], top_part[1]);
+        n_top = top_part[2];
+    };
 
     if (warp == WARPS) {                      // the teacher
-        const auto prepare = [&](int64_t t, int buf) {
-            int* const slot = slots + buf * K;
-            float* const lq = lqs + buf * K;
-            const float w = a.weights ? a.weights[t] : 1.0f, lse = tail ? a.teacher_lse[t] : 0.0f;
+        float s_t_next = 0.0f, w_next = 0.0f;
+        bool twice_next = false;
+        int64_t last = -1, before = -1;
+        for (int i = lane; i < (slice_vecs * VE + 31) / 32; i += 32) bits[i] = 0;
+        __syncwarp();
+        const auto prepare = [&](int64_t t, int p) {
+            int* const slot = slots + p * K;
+            float* const lq = lqs + p * K;
+            float s_t = 0.0f;
+            w_next = a.weights ? a.weights[t] : 1.0f;
+            const float lse = tail ? a.teacher_lse[t] : 0.0f;
             const Slice<T> sl(a, t, rank, log_cluster);
-            float tmax = -INFINITY, s_t = 0.0f;
+            float tmax = -INFINITY;
+            uint32_t seen = 0;
+#pragma unroll 2
             for (int k = lane; k < K; k += 32) {
                 const int64_t id = a.ids64 ? static_cast<const int64_t*>(a.ids)[t * K + k] : static_cast<const int32_t*>(a.ids)[t * K + k];
                 float tl = load_f32(a.top_logits, a.top_dtype, t * K + k);
                 if (id < 0 || id >= V) tl = -INFINITY;
-                slot[k] = id >= sl.j0 && id < sl.j1 ? (int)id - sl.e0 : -1;
+                const int e = id >= sl.j0 && id < sl.j1 ? (int)id - sl.e0 : -1;
+                slot[k] = e;
                 lq[k] = tl;
                 tmax = fmaxf(tmax, tl);
+                if (e >= 0) seen |= atomicOr(&bits[e >> 5], 1u << (e & 31)) & (1u << (e & 31));
             }
+            twice_next = __any_sync(0xffffffffu, seen != 0);
             tmax = finite_ref(warp_max1(tmax));
             for (int k = lane; k < K; k += 32) {
+                if (slot[k] >= 0) bits[slot[k] >> 5] = 0;
                 const float tl = lq[k];
                 // -infinity stays: its products with the two parts of 1 / tau could cancel to NaN
                 const float l = tl == -INFINITY ? tl : tail ? __fmaf_rn(tl, a.inv_tau, __fmaf_rn(tl, a.inv_tau_lo, -lse)) : (tl - tmax) * a.inv_tau;
                 lq[k] = l;
                 s_t += expf(l);
             }
-            s_t = warp_sum(s_t);
+            s_t = sum_lanes<32>(s_t);
             if (!tail && s_t > 0.0f) {
                 const float log_t = logf(s_t);
                 for (int k = lane; k < K; k += 32) lq[k] -= log_t;
             }
-            if (lane == 0) { teacher[buf][0] = s_t; teacher[buf][1] = w; }
+            s_t_next = s_t;
+            __syncwarp();
         };
         if (t < a.tokens) prepare(t, 0);
         while (t < a.tokens) {
+            const int* const slot = slots + parity * K;
+            const float* const lq = lqs + parity * K;
+            const float s_t = s_t_next, w = w_next;
+            const bool twice = twice_next;
+            const Slice<T> sl(a, t, rank, log_cluster);
+            T* const g = GRAD ? static_cast<T*>(a.grad) + t * a.grad_stride + sl.e0 : nullptr;
             const float ahead = weight_ahead(a, t + step, step);
-            row_ready<THREADS>();
+            if (lane == 0) { teacher[0] = s_t; teacher[1] = w; }
+            meet<THREADS>(B_ROW);
+            float m_top = -INFINITY, s_top = 0.0f, n_top = 0.0f;
+            for (int k = lane; k < K; k += 32)
+                if (const int e = slot[k]; e >= 0) m_top = fmaxf(m_top, zk[k] = to_f32(elem[e]));
+            __syncwarp();
+            for (int k = lane; k < K; k += 32)
+                if (const int e = slot[k]; e >= 0) reinterpret_cast<typename Row<T>::Bits*>(elem)[e] = Row<T>::minus_inf;
+            pass<THREADS>(B_TAKEN);
+            m_top = warp_max1(m_top);
+            for (int k = lane; k < K; k += 32) {
+                const int e = slot[k];
+                if (e < 0) continue;
+                bool first = true;       // every id counts once
+                if (twice) for (int i = 0; i < k; ++i) first &= slot[i] != e;
+                if (first) {
+                    s_top += ex2((zk[k] - finite_ref(m_top)) * c);
+                    n_top += 1.0f;
+                }
+            }
+            s_top = sum_lanes<32>(s_top);
+            n_top = sum_lanes<32>(n_top);
+            if (lane == 0) { top_part[0] = m_top; top_part[1] = s_top; top_part[2] = n_top; }
+            pass<THREADS>(B_PARTS);
             if (log_cluster) cluster_arrive();
+            last = t;
             t = live_row(a, t + step, step, ahead);
-            if (t < a.tokens) prepare(t, buf ^= 1);
-            if (log_cluster) { cluster_wait(); cluster_barrier(); }
+            if (t < a.tokens) prepare(t, parity ^ 1);
+            float2 rest, top;
+            if (log_cluster) {
+                cluster_wait();
+                if (rank == 0 && before >= 0) {        // the row before: its shares of the loss have arrived
+                    const float l = sum_lanes<kMaxCluster>(lane < cluster ? loss_ranks[parity ^ 1][lane] : 0.0f);
+                    if (lane == 0) a.loss[before] = l;
+                }
+                joined(rest, top, n_top);
+            } else {
+                meet<THREADS>(B_PARTS_SEEN);
+                own_classes(rest, top, n_top);
+            }
+            const RowSums r(rest, top, n_top, s_t, c, tail, V);
+            const float log_s = logf(r.s);
+            float l = 0.0f;
+            for (int k = lane; k < K; k += 32) {
+                if (slot[k] < 0) continue;
+                const float q = expf(lq[k]);
+                if (q != 0.0f) l += q * (lq[k] - (zk[k] == -INFINITY && r.s == r.s ? -INFINITY : (zk[k] - r.m) * a.inv_tau - log_s));
+            }
+            l = sum_lanes<32>(l);
+            if (rank == 0 && r.q_rest > 0.0f)
+                l += r.q_rest * (logf(r.q_rest) - (r.s_rest > 0.0f ? (r.m_rest - r.m) * a.inv_tau + logf(r.s_rest) - log_s : -INFINITY));
+            if (lane == 0) {
+                if (log_cluster) store_at(&loss_ranks[parity][rank], 0, w * l);
+                else a.loss[last] = w * l;
+            }
+            if constexpr (GRAD) {
+                const float scale = w * a.inv_tau, q_scale = r.Q * r.inv_s * scale;
+                for (int k = lane; k < K; k += 32) {
+                    const int e = slot[k];
+                    float q = 0.0f;
+                    if (e >= 0 && twice) {
+                        for (int i = 0; i < K; ++i) if (slot[i] == e) q += expf(lq[i]);
+                    } else {
+                        q = expf(lq[k]);
+                    }
+                    zk[k] = __fmaf_rn(ex2((zk[k] - r.m) * c), q_scale, -q * scale);
+                }
+                meet<THREADS>(B_WRITTEN);
+                for (int k = lane; k < K; k += 32) if (const int e = slot[k]; e >= 0) g[e] = from_f32<T>(zk[k]);
+            }
+            before = last;
+            parity ^= 1;
+        }
+        if (log_cluster) {
+            cluster_barrier();
+            if (rank == 0 && last >= 0) {
+                const float l = sum_lanes<kMaxCluster>(lane < cluster ? loss_ranks[parity ^ 1][lane] : 0.0f);
+                if (lane == 0) a.loss[last] = l;
+            }
         }
         return;
     }
@@ -246,47 +370,14 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
         }
     }
 
-    for (; t < a.tokens; buf ^= 1) {
-        const int* const slot = slots + buf * K;
-        const float* const lq = lqs + buf * K;
+    while (t < a.tokens) {
         const Slice<T> sl(a, t, rank, log_cluster);
         const int nv = sl.nv;
         const float ahead = weight_ahead(a, t + step, step);
         copies_landed();
-        row_ready<THREADS>();
-        const float s_t = teacher[buf][0], w = teacher[buf][1];
-        // The listed entries of this slice leave it. An entry first puts its number into its element: where it then finds
-        // another one, an id is listed twice.
-        int twice = 0;
-        if (entries) {
-            const auto together = [&] { asm volatile("bar.sync 1, %0;" ::"r"(estride) : "memory"); };
-            float m_top = -INFINITY, s_top = 0.0f, n_top = 0.0f;
-            for (int k = tid; k < K; k += estride) {
-                const int e = slot[k];
-                if (e >= 0) m_top = fmaxf(m_top, zk[k] = to_f32(reinterpret_cast<const T*>(elem)[e]));
-            }
-            m_top = warp_max1(m_top);
-            together();
-            for (int k = tid; k < K; k += estride) if (const int e = slot[k]; e >= 0) elem[e] = (Bits)k;
-            together();
-            for (int k = tid; k < K; k += estride) if (const int e = slot[k]; e >= 0) twice |= elem[e] != (Bits)k;
-            asm volatile("{\n.reg .pred p, q;\nsetp.ne.s32 p, %1, 0;\nbar.red.or.pred q, 1, %2, p;\nselp.s32 %0, 1, 0, q;\n}" : "=r"(twice) : "r"(twice), "r"(estride) : "memory");
-            for (int k = tid; k < K; k += estride) {
-                const int e = slot[k];
-                if (e < 0) continue;
-                elem[e] = Row<T>::minus_inf;
-                bool first = true;       // every id counts once
-                if (twice) for (int i = 0; i < k; ++i) first &= slot[i] != e;
-                if (first) {
-                    s_top += ex2((zk[k] - finite_ref(m_top)) * c);
-                    n_top += 1.0f;
-                }
-            }
-            s_top = warp_sum(s_top);
-            n_top = warp_sum(n_top);
-            if (lane == 0) { part[warp][P_MTOP] = m_top; part[warp][P_STOP] = s_top; part[warp][P_NTOP] = n_top; }
-        }
-        workers_together<THREADS>();
+        meet<THREADS>(B_ROW);
+        const float s_t = teacher[0], w = teacher[1];
+        meet<THREADS>(B_TAKEN);
         const int64_t t_next = live_row(a, t + step, step, ahead);
         const Slice<T> next(a, min(t_next, a.tokens - 1), rank, log_cluster);
         const int nv_next = t_next < a.tokens ? next.nv : 0;
@@ -308,140 +399,84 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
                 }
             }
             if constexpr (!GRAD) for (int v = tid; v < nv_next; v += THREADS) next.fetch(vec, v, V);
-            const float s = warp_sum(sum.x + sum.y);
-            if (lane == 0) { part[warp][P_MREST] = m; part[warp][P_SREST] = s; }
+            const float s = sum_lanes<32>(sum.x + sum.y);
+            if (lane == 0) { part[warp][0] = m; part[warp][1] = s; }
         }
-        workers_together<THREADS>();
-        float2 rest, top;
-        float n_top;
-        {
-            bool in = lane < WARPS;
-            rest = join_lanes(in ? part[lane][P_MREST] : -INFINITY, in ? part[lane][P_SREST] : 0.0f, c);
-            in = lane < entry_warps;
-            top = join_lanes(in ? part[lane][P_MTOP] : -INFINITY, in ? part[lane][P_STOP] : 0.0f, c);
-            n_top = warp_sum(in ? part[lane][P_NTOP] : 0.0f);
-        }
-        if (log_cluster) {
-            if (tid < cluster) {
-                float* const mine = ranks[rank];
-                store_at(mine + P_MREST, tid, rest.x); store_at(mine + P_SREST, tid, rest.y);
-                store_at(mine + P_MTOP, tid, top.x); store_at(mine + P_STOP, tid, top.y); store_at(mine + P_NTOP, tid, n_top);
+        meet<THREADS>(B_PARTS);
+        if (!log_cluster) pass<THREADS>(B_PARTS_SEEN);
+        if (GRAD || log_cluster) {
+            float2 rest, top;
+            float n_top;
+            own_classes(rest, top, n_top);
+            if (log_cluster) {
+                if (tid < cluster) {
+                    float* const mine = ranks[parity][rank];
+                    store_at(mine, tid, rest.x); store_at(mine + 1, tid, rest.y);
+                    store_at(mine + 2, tid, top.x); store_at(mine + 3, tid, top.y); store_at(mine + 4, tid, n_top);
+                }
+                cluster_barrier();
+                if constexpr (GRAD) joined(rest, top, n_top);
             }
-            cluster_barrier();
-            const bool in = lane < cluster;
-            const float* const r = ranks[in ? lane : 0];
-            rest = join_lanes(in ? r[P_MREST] : -INFINITY, in ? r[P_SREST] : 0.0f, c);
-            top = join_lanes(in ? r[P_MTOP] : -INFINITY, in ? r[P_STOP] : 0.0f, c);
-            n_top = warp_sum(in ? r[P_NTOP] : 0.0f);
-        }
-        const float m_rest = rest.x, s_rest = rest.y, m = finite_ref(fmaxf(m_rest, top.x));
-        const float f_rest = ex2((m_rest - m) * c);                    // 0 when nothing is left out
-        const float s = __fmaf_rn(s_rest, f_rest, top.y * ex2((top.x - m) * c));
-        const float inv_s = s > 0.0f || s != s ? 1.0f / s : 0.0f;
-        const float q_rest = tail && n_top < (float)V ? fmaxf(1.0f - s_t, 0.0f) : 0.0f;
-        const float Q = tail ? s_t + q_rest : (s_t > 0.0f || s_t != s_t) ? 1.0f : 0.0f;
-        const float scale = w * a.inv_tau;
-        if (entries) {      // this slice's share of the loss
-            const float log_s = logf(s);
-            float l = 0.0f;
-            for (int k = tid; k < K; k += estride) {
-                if (slot[k] < 0) continue;
-                const float q = expf(lq[k]);
-                if (q != 0.0f) l += q * (lq[k] - (zk[k] == -INFINITY && s == s ? -INFINITY : (zk[k] - m) * a.inv_tau - log_s));
-            }
-            l = warp_sum(l);
-            if (tid == 0 && rank == 0 && q_rest > 0.0f)
-                l += q_rest * (logf(q_rest) - (s_rest > 0.0f ? (m_rest - m) * a.inv_tau + logf(s_rest) - log_s : -INFINITY));
-            if (lane == 0) loss_part[warp] = l;
-        }
-        bool fetched = !GRAD;
-        T* const g = GRAD ? static_cast<T*>(a.grad) + t * a.grad_stride : nullptr;
-        if constexpr (GRAD) {
-            // Left out: p_j (Q - q_rest / p_rest) with p_j = 2^(c (z_j - m_rest)) f_rest / s and p_rest = s_rest f_rest / s.
-            const float coef = (Q * f_rest * inv_s - (s_rest > 0.0f ? q_rest / s_rest : 0.0f)) * scale;
-            const float2 neg = splat(-finite_ref(m_rest)), c2 = splat(c), coef2 = splat(coef);
-            if ((reinterpret_cast<uintptr_t>(g) - reinterpret_cast<uintptr_t>(sl.z)) % 16 == 0) {
-                uint4* const dst = reinterpret_cast<uint4*>(g + sl.e0);
-                for (int v = tid; v < nv; v += THREADS) {
-                    float2 x[VE / 2];
-                    to_pairs<T>(vec[v], x);
+            if constexpr (GRAD) {
+                const RowSums r(rest, top, n_top, s_t, c, tail, V);
+                T* const g = static_cast<T*>(a.grad) + t * a.grad_stride;
+                // Left out: p_j (Q - q_rest / p_rest) with p_j = 2^(c (z_j - m_rest)) f_rest / s and p_rest = s_rest f_rest / s.
+                const float coef = (r.Q * r.f_rest * r.inv_s - (r.s_rest > 0.0f ? r.q_rest / r.s_rest : 0.0f)) * (w * a.inv_tau);
+                const float2 neg = splat(-finite_ref(r.m_rest)), c2 = splat(c), coef2 = splat(coef);
+                if ((reinterpret_cast<uintptr_t>(g) - reinterpret_cast<uintptr_t>(sl.z)) % 16 == 0) {
+                    uint4* const dst = reinterpret_cast<uint4*>(g + sl.e0);
+                    for (int v = tid; v < nv; v += THREADS) {
+                        float2 x[VE / 2];
+                        to_pairs<T>(vec[v], x);
 #pragma unroll
-                    for (int i = 0; i < VE / 2; ++i) {
-                        const float2 y = mul2_rn(add2_rn(x[i], neg), c2);
-                        x[i] = mul2_rn(make_float2(ex2(y.x), ex2(y.y)), coef2);
-                    }
-                    if (v < nv_next) next.fetch(vec, v, V);
-                    if (v >= sl.whole0 && v < sl.whole1) {
-                        dst[v] = from_pairs<T>(x);
-                    } else {
+                        for (int i = 0; i < VE / 2; ++i) {
+                            const float2 y = mul2_rn(add2_rn(x[i], neg), c2);
+                            x[i] = mul2_rn(make_float2(ex2(y.x), ex2(y.y)), coef2);
+                        }
+                        if (v < nv_next) next.fetch(vec, v, V);
+                        if (v >= sl.whole0 && v < sl.whole1) {
+                            dst[v] = from_pairs<T>(x);
+                        } else {
 #pragma unroll
-                        for (int i = 0; i < VE; ++i) {
-                            const int j = sl.e0 + v * VE + i;
-                            if (j >= 0 && j < V) g[j] = from_f32<T>(i & 1 ? x[i / 2].y : x[i / 2].x);
+                            for (int i = 0; i < VE; ++i) {
+                                const int j = sl.e0 + v * VE + i;
+                                if (j >= 0 && j < V) g[j] = from_f32<T>(i & 1 ? x[i / 2].y : x[i / 2].x);
+                            }
                         }
                     }
-                }
-                // the next row may have a vector more
-                for (int v = tid + (nv - tid + THREADS - 1) / THREADS * THREADS; v < nv_next; v += THREADS) next.fetch(vec, v, V);
-                fetched = true;
-            } else {
-                // The gradient's rows are aligned otherwise than the logits': its own vectors, gathered element by element.
-                const int goff = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T));
-                const int u1 = (sl.j1 + goff + VE - 1) / VE;
+                    // the next row may have a vector more
+                    for (int v = tid + (nv - tid + THREADS - 1) / THREADS * THREADS; v < nv_next; v += THREADS) next.fetch(vec, v, V);
+                    pass<THREADS>(B_WRITTEN);
+                } else {
+                    // The gradient's rows are aligned otherwise than the logits': its own vectors, gathered element by element.
+                    const int goff = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T));
+                    const int u1 = (sl.j1 + goff + VE - 1) / VE;
 #pragma unroll 1
-                for (int u = (sl.j0 + goff) / VE + tid; u < u1; u += THREADS) {
-                    const int j = u * VE - goff;
-                    float2 x[VE / 2];
+                    for (int u = (sl.j0 + goff) / VE + tid; u < u1; u += THREADS) {
+                        const int j = u * VE - goff;
+                        float2 x[VE / 2];
 #pragma unroll
-                    for (int i = 0; i < VE; ++i) {
-                        const float zi = j + i >= sl.j0 && j + i < sl.j1 ? to_f32(reinterpret_cast<const T*>(elem)[j + i - sl.e0]) : -INFINITY;
-                        (i & 1 ? x[i / 2].y : x[i / 2].x) = ex2((zi + neg.x) * c) * coef;
-                    }
-                    if (j >= sl.j0 && j + VE <= sl.j1) {
-                        *reinterpret_cast<uint4*>(g + j) = from_pairs<T>(x);
-                    } else {
+                        for (int i = 0; i < VE; ++i) {
+                            const float zi = j + i >= sl.j0 && j + i < sl.j1 ? to_f32(elem[j + i - sl.e0]) : -INFINITY;
+                            (i & 1 ? x[i / 2].y : x[i / 2].x) = ex2((zi + neg.x) * c) * coef;
+                        }
+                        if (j >= sl.j0 && j + VE <= sl.j1) {
+                            *reinterpret_cast<uint4*>(g + j) = from_pairs<T>(x);
+                        } else {
 #pragma unroll
-                        for (int i = 0; i < VE; ++i)
-                            if (j + i >= sl.j0 && j + i < sl.j1) g[j + i] = from_f32<T>(i & 1 ? x[i / 2].y : x[i / 2].x);
+                            for (int i = 0; i < VE; ++i)
+                                if (j + i >= sl.j0 && j + i < sl.j1) g[j + i] = from_f32<T>(i & 1 ? x[i / 2].y : x[i / 2].x);
+                        }
                     }
+                    meet<THREADS>(B_WRITTEN);
+                    for (int v = tid; v < nv_next; v += THREADS) next.fetch(vec, v, V);
                 }
-            }
-        }
-        workers_together<THREADS>();        // the listed entries' gradients go over the slice's, and the warps' shares of the loss are there
-        if (!fetched) for (int v = tid; v < nv_next; v += THREADS) next.fetch(vec, v, V);
-        if constexpr (GRAD) {
-            if (entries) {
-                const float q_scale = Q * inv_s * scale;
-                for (int k = tid; k < K; k += estride) {
-                    const int e = slot[k];
-                    if (e < 0) continue;
-                    float q = 0.0f;
-                    if (twice) {
-                        for (int i = 0; i < K; ++i) if (slot[i] == e) q += expf(lq[i]);
-                    } else {
-                        q = expf(lq[k]);
-                    }
-                    g[sl.e0 + e] = from_f32<T>(__fmaf_rn(ex2((zk[k] - m) * c), q_scale, -q * scale));
-                }
-            }
-        }
-        if (warp == 0) {
-            const float l = warp_sum(lane < entry_warps ? loss_part[lane] : 0.0f);
-            if (lane == 0) {
-                if (log_cluster) store_at(&ranks[rank][P_COUNT], 0, l);
-                else a.loss[t] = w * l;
-            }
-        }
-        if (log_cluster) {
-            cluster_barrier();
-            if (rank == 0 && tid == 0) {
-                float l = 0.0f;
-                for (int r = 0; r < cluster; ++r) l += ranks[r][P_COUNT];
-                a.loss[t] = w * l;
             }
         }
         t = t_next;
+        parity ^= 1;
     }
+    if (log_cluster) cluster_barrier();
 }
 
 template <typename T, int THREADS, bool GRAD>
@@ -464,7 +499,7 @@ cudaError_t launch(const DistillArgs& a, int log_cluster, int slice_vecs, size_t
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = cluster > 1 ? 1 : 0;
-    e = cudaLaunchKernelEx(&cfg, kernel, a, log_cluster, slice_vecs, std::min(THREADS / 32, (a.top + 63) / 64));
+    e = cudaLaunchKernelEx(&cfg, kernel, a, log_cluster, slice_vecs);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -479,7 +514,7 @@ cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, cudaStream_t 
     while (log_cluster < 3 && row_vecs > (int64_t)4096 << log_cluster) ++log_cluster;
     while (log_cluster < 3 && a.tokens << log_cluster < 148 && row_vecs > (int64_t)1024 << log_cluster) ++log_cluster;
     const int slice = (int)((row_vecs + (1 << log_cluster) - 1) >> log_cluster) + 1;
-    const size_t bytes = (size_t)slice * 16 + (size_t)a.top * 20;
+    const size_t bytes = (size_t)slice * 16 + (size_t)a.top * 20 + ((size_t)slice * 16 / es + 31) / 32 * 4;
     return with_dtype(logits_dtype, [&](auto t) {
         using T = decltype(t);
         if (slice <= 1024) return a.grad ? launch<T, 128, true>(a, log_cluster, slice, bytes, s) : launch<T, 128, false>(a, log_cluster, slice, bytes, s);
