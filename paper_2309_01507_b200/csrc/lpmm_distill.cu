@@ -20,7 +20,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxCluster = 8;
-constexpr int blocks_per_sm(int threads) { return threads == 256 ? 3 : 8; }
+constexpr int blocks_per_sm(int threads) { return 1024 / threads; }
 
 __device__ __forceinline__ float ex2(float x) {
     float r;
@@ -381,6 +381,9 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
         const int64_t t_next = live_row(a, t + step, step, ahead);
         const Slice<T> next(a, min(t_next, a.tokens - 1), rank, log_cluster);
         const int nv_next = t_next < a.tokens ? next.nv : 0;
+        const auto fetch_more = [&] {      // the next row may have a vector more than this one
+            for (int v = tid + (nv - tid + THREADS - 1) / THREADS * THREADS; v < nv_next; v += THREADS) next.fetch(vec, v, V);
+        };
         {
             VecMax<T> vm;
 #pragma unroll 4
@@ -392,13 +395,14 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
             for (int v = tid; v < nv; v += THREADS) {
                 float2 x[VE / 2];
                 to_pairs<T>(vec[v], x);
+                if (!GRAD && v < nv_next) next.fetch(vec, v, V);
 #pragma unroll
                 for (int i = 0; i < VE / 2; ++i) {
                     const float2 y = mul2_rn(add2_rn(x[i], neg), c2);
                     sum = add2_rn(sum, make_float2(ex2(y.x), ex2(y.y)));
                 }
             }
-            if constexpr (!GRAD) for (int v = tid; v < nv_next; v += THREADS) next.fetch(vec, v, V);
+            if constexpr (!GRAD) fetch_more();
             const float s = sum_lanes<32>(sum.x + sum.y);
             if (lane == 0) { part[warp][0] = m; part[warp][1] = s; }
         }
@@ -444,8 +448,7 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
                             }
                         }
                     }
-                    // the next row may have a vector more
-                    for (int v = tid + (nv - tid + THREADS - 1) / THREADS * THREADS; v < nv_next; v += THREADS) next.fetch(vec, v, V);
+                    fetch_more();
                     pass<THREADS>(B_WRITTEN);
                 } else {
                     // The gradient's rows are aligned otherwise than the logits': its own vectors, gathered element by element.
@@ -508,17 +511,18 @@ cudaError_t launch(const DistillArgs& a, int log_cluster, int slice_vecs, size_t
 cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, cudaStream_t s) {
     const int64_t es = logits_dtype == 0 ? 4 : 2;
     const int64_t row_vecs = a.vocab * es / 16 + 2;    // however the row is aligned
-    // Slices of up to 64 KB, three of which an SM holds at a time; eight CTAs at most. Few rows are split further, until every
-    // SM has a CTA or a slice is down to 8 KB.
+    // A CTA takes a whole row where its shared memory holds one; the CTAs of a cluster wait for one another twice per row, which
+    // costs more than it gains. Few rows are split, until every SM has a CTA or a slice is down to 8 KB.
     int log_cluster = 0;
-    while (log_cluster < 3 && row_vecs > (int64_t)4096 << log_cluster) ++log_cluster;
+    while (log_cluster < 3 && row_vecs > (int64_t)12800 << log_cluster) ++log_cluster;
     while (log_cluster < 3 && a.tokens << log_cluster < 148 && row_vecs > (int64_t)1024 << log_cluster) ++log_cluster;
     const int slice = (int)((row_vecs + (1 << log_cluster) - 1) >> log_cluster) + 1;
     const size_t bytes = (size_t)slice * 16 + (size_t)a.top * 20 + ((size_t)slice * 16 / es + 31) / 32 * 4;
     return with_dtype(logits_dtype, [&](auto t) {
         using T = decltype(t);
         if (slice <= 1024) return a.grad ? launch<T, 128, true>(a, log_cluster, slice, bytes, s) : launch<T, 128, false>(a, log_cluster, slice, bytes, s);
-        return a.grad ? launch<T, 256, true>(a, log_cluster, slice, bytes, s) : launch<T, 256, false>(a, log_cluster, slice, bytes, s);
+        if (slice <= 4352) return a.grad ? launch<T, 256, true>(a, log_cluster, slice, bytes, s) : launch<T, 256, false>(a, log_cluster, slice, bytes, s);
+        return a.grad ? launch<T, 512, true>(a, log_cluster, slice, bytes, s) : launch<T, 512, false>(a, log_cluster, slice, bytes, s);
     });
 }
 
