@@ -1279,7 +1279,7 @@ bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p
 
 lpmm_status check_w4(const lpmm_w4* m) {
     if (!m || !m->d_codes || !m->d_scales || m->rows <= 0 || m->cols <= 0 || !known_dtype(m->scale_dtype)) return LPMM_ERR_INVALID_ARG;
-    if (m->rows > ((int64_t)1 << 40) / m->cols || m->cols > INT32_MAX / 2) return LPMM_ERR_INVALID_ARG;
+    if (m->rows > ((int64_t)1 << 40) / m->cols || m->cols > INT32_MAX / 2 || m->rows > INT32_MAX / 2) return LPMM_ERR_INVALID_ARG;
     if (m->codes_stride < (m->cols + 1) / 2 || m->codes_stride > ((int64_t)1 << 40) / m->rows) return LPMM_ERR_INVALID_ARG;
     if (m->group != 32 && m->group != 64 && (m->group <= 0 || m->group % 128 != 0)) return LPMM_ERR_UNSUPPORTED;
     if (m->codes_stride % 16 != 0 || !aligned16(m->d_codes) || !aligned_to(m->d_scales, dtype_bytes(m->scale_dtype))) return LPMM_ERR_ALIGNMENT;
