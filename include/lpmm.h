@@ -282,7 +282,9 @@ lpmm_status lpmm_w4_dequantize(const lpmm_w4* m, void* d_out, int32_t out_dtype,
  * (0: nothing to do). One read of the codes serves a block of tokens, so it is meant for single tokens and
  * small batches; it is right for any number.
  *   x_dtype  LPMM_F32, LPMM_BF16 or LPMM_F16; y_dtype the same, or LPMM_F32. d_bias: rows floats, or NULL.
- *   x_stride >= cols, y_stride >= rows; d_x and d_y need the alignment of their elements only. */
+ *   x_stride >= cols, y_stride >= rows; d_x and d_y need the alignment of their elements only.
+ * cols <= LPMM_W4_MAX_COLS, else LPMM_ERR_UNSUPPORTED. Results are the same bits every time. */
+#define LPMM_W4_MAX_COLS 131072
 lpmm_status lpmm_w4_matvec(const lpmm_w4* m, const void* d_x, int32_t x_dtype, int64_t x_stride, int64_t tokens,
                            const float* d_bias, void* d_y, int32_t y_dtype, int64_t y_stride, void* stream);
 

@@ -1280,7 +1280,7 @@ bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p
 lpmm_status check_w4(const lpmm_w4* m) {
     if (!m || !m->d_codes || !m->d_scales || m->rows <= 0 || m->cols <= 0 || !known_dtype(m->scale_dtype)) return LPMM_ERR_INVALID_ARG;
     if (m->rows > ((int64_t)1 << 40) / m->cols || m->cols > INT32_MAX / 2 || m->rows > INT32_MAX / 2) return LPMM_ERR_INVALID_ARG;
-    if (m->codes_stride < (m->cols + 1) / 2 || m->codes_stride > ((int64_t)1 << 40) / m->rows) return LPMM_ERR_INVALID_ARG;
+    if (m->codes_stride < (m->cols + 1) / 2 || m->codes_stride > 1 << 27) return LPMM_ERR_INVALID_ARG;
     if (m->group != 32 && m->group != 64 && (m->group <= 0 || m->group % 128 != 0)) return LPMM_ERR_UNSUPPORTED;
     if (m->codes_stride % 16 != 0 || !aligned16(m->d_codes) || !aligned_to(m->d_scales, dtype_bytes(m->scale_dtype))) return LPMM_ERR_ALIGNMENT;
     return LPMM_OK;
@@ -1341,6 +1341,7 @@ lpmm_status lpmm_w4_matvec(const lpmm_w4* m, const void* d_x, int32_t x_dtype, i
     lpmm_status rc = check_w4(m);
     if (rc != LPMM_OK) return rc;
     if (tokens < 0 || !known_dtype(x_dtype) || (y_dtype != x_dtype && y_dtype != LPMM_F32)) return LPMM_ERR_INVALID_ARG;
+    if (m->cols > LPMM_W4_MAX_COLS) return LPMM_ERR_UNSUPPORTED;
     if (tokens == 0) return LPMM_OK;
     rc = check_rows(d_x, x_dtype, tokens, m->cols, x_stride);
     if (rc == LPMM_OK) rc = check_rows(d_y, y_dtype, tokens, m->rows, y_stride);

@@ -143,17 +143,18 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
 // scale is applied once per group to their result. fp32 activations enter as three bfloat16 parts that add up to them exactly
 // (8 significant bits each), as three columns instead of one.
 //
-// A warp owns 16 rows and streams its codes through a ring of its own in shared memory (cp.async, 256 columns = 2 KB per stage),
-// so nothing in the loop waits for another warp. A lane reads one 32-bit word = 8 codes of one row per 32 columns; the pairs
-// that its halves hold, (0, 4), (1, 5), (2, 6), (3, 7), are brought to the tensor cores' operand by a mask, an OR with the
-// exponent of a power of two and one exact subtraction. The order of the columns inside a product is free as long as both
-// operands have the same: the activations are put into shared memory with their pairs in that order.
+// One CTA per SM holds the activations in shared memory and goes through tiles of 16 rows; its warps share out the stages (16 rows
+// by 512 columns, 4 KB of codes) of all its tiles evenly, in order, each streaming its own through two buffers of its own in
+// shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. A lane reads one 32-bit word =
+// 8 codes of one row per 32 columns; the pairs that its halves hold, (0, 4), (1, 5), (2, 6), (3, 7), are brought to the tensor
+// cores' operand by a mask and one exact multiply-add. The order of the columns inside a product is free as long as both operands
+// have the same: the activations' pairs are put into that order.
 //
-// The columns of a row tile are split over the CTAs of a cluster when there are fewer tiles than the SMs can hold; the ranks'
-// sums are added in rank order through distributed shared memory, so results are the same bits every time.
+// A tile's sums from the warps that share it, and from the CTAs of a cluster, which split the columns when the activations do not
+// fit one CTA or the tiles are few, are added in a fixed order at the end: results are the same bits every time.
 
-constexpr int kStageCols = 256, kStageBytes = kStageCols / 2;   // columns of one ring stage; its bytes per row
-constexpr int kStages = 4;
+constexpr int kStageCols = 512, kStageBytes = kStageCols / 2;   // columns of one stage; its bytes per row
+constexpr int kStages = 2;
 constexpr int kWarpRing = kStages * 16 * kStageBytes;           // 8 KB
 constexpr int kXPad = 64;                                       // bytes between columns: neighbouring columns on other banks
 
@@ -174,26 +175,30 @@ __device__ __forceinline__ float ld_rank(uint32_t a, uint32_t rank) {    // the 
     return v;
 }
 
-// Eight codes as four operand registers: (q0, q4), (q1, q5), (q2, q6), (q3, q7), minus the zero point. `zero` and `zero16` come
-// from zero_operand().
+// Eight codes as four operand registers: (q0, q4), (q1, q5), (q2, q6), (q3, q7), minus the zero point and times `unit`. `zero` and
+// `zero16` come from zero_operand().
 template <typename M> struct Codes;
 template <> struct Codes<__half> {
+    static constexpr float unit = 1.0f;
     // 0x6400 is 1024: OR-ing a code into its low bits adds it, into bits 4-7 adds 16 times it.
     __device__ __forceinline__ static void zero_operand(float z, uint32_t& zero, uint32_t& zero16) {
-        zero = pack_pair<__half>(1024.0f + z, 1024.0f + z);
+        zero = pack_pair<__half>(-1024.0f - z, -1024.0f - z);
         zero16 = pack_pair<__half>(-64.0f - z, -64.0f - z);
     }
     __device__ __forceinline__ static void expand(uint32_t w, uint32_t zero, uint32_t zero16, uint32_t (&o)[4]) {
-        const uint32_t w8 = w >> 8, sixteenth = 0x2c002c00u;
-        uint32_t t[4];
-        asm("lop3.b32 %0, %1, 0x000f000f, 0x64006400, 0xEA;" : "=r"(t[0]) : "r"(w));
-        asm("lop3.b32 %0, %1, 0x00f000f0, 0x64006400, 0xEA;" : "=r"(t[1]) : "r"(w));
-        asm("lop3.b32 %0, %1, 0x000f000f, 0x64006400, 0xEA;" : "=r"(t[2]) : "r"(w8));
-        asm("lop3.b32 %0, %1, 0x00f000f0, 0x64006400, 0xEA;" : "=r"(t[3]) : "r"(w8));
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(o[0]) : "r"(t[0]), "r"(zero));
-        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(o[1]) : "r"(t[1]), "r"(sixteenth), "r"(zero16));
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(o[2]) : "r"(t[2]), "r"(zero));
-        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(o[3]) : "r"(t[3]), "r"(sixteenth), "r"(zero16));
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            uint32_t lo, hi;
+            asm("lop3.b32 %0, %1, 0x000f000f, 0x64006400, 0xEA;" : "=r"(lo) : "r"(w));
+            asm("lop3.b32 %0, %1, 0x00f000f0, 0x64006400, 0xEA;" : "=r"(hi) : "r"(w));
+            asm("add.rn.f16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(lo), "r"(zero));
+            asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(o[i + 1]) : "r"(hi), "r"(0x2c002c00u), "r"(zero16));    // 1/16
+            w >>= 8;
+        }
+    }
+    __device__ __forceinline__ static void mma0(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {    // the first of a sum
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
     }
     __device__ __forceinline__ static void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -201,18 +206,27 @@ template <> struct Codes<__half> {
     }
 };
 template <> struct Codes<__nv_bfloat16> {
-    // 0x4300 is 128 with seven bits of mantissa: only a code in the low four bits fits.
+    static constexpr float unit = 0.25f;
+    // Low code: 0x4300 is 128 with seven bits of mantissa, 128 + q. High code, in bits 4-7: below two smallest normal numbers the
+    // bits of a bfloat16 count multiples of 2^-133, so the bits alone are 16 q 2^-133 = q 2^-129, which 2^127 brings to q / 4.
+    // Neither needs a shift; both end as (q - z) / 4.
     __device__ __forceinline__ static void zero_operand(float z, uint32_t& zero, uint32_t& zero16) {
-        zero = pack_pair<__nv_bfloat16>(128.0f + z, 128.0f + z);
-        zero16 = 0;
+        zero = pack_pair<__nv_bfloat16>(-32.0f - 0.25f * z, -32.0f - 0.25f * z);
+        zero16 = pack_pair<__nv_bfloat16>(-0.25f * z, -0.25f * z);
     }
-    __device__ __forceinline__ static void expand(uint32_t w, uint32_t zero, uint32_t, uint32_t (&o)[4]) {
+    __device__ __forceinline__ static void expand(uint32_t w, uint32_t zero, uint32_t zero16, uint32_t (&o)[4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t t;
-            asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xEA;" : "=r"(t) : "r"(w >> (4 * i)));
-            asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(t), "r"(zero));
+        for (int i = 0; i < 4; i += 2) {
+            uint32_t lo, hi = w & 0x00f000f0u;
+            asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xEA;" : "=r"(lo) : "r"(w));
+            asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(o[i]) : "r"(lo), "r"(0x3e803e80u), "r"(zero));           // 1/4
+            asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(o[i + 1]) : "r"(hi), "r"(0x7f007f00u), "r"(zero16));    // 2^127
+            w >>= 8;
         }
+    }
+    __device__ __forceinline__ static void mma0(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {    // the first of a sum
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
     }
     __device__ __forceinline__ static void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
         asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -231,16 +245,36 @@ struct W4Product {
     int64_t y_stride;
     int32_t scale_dtype, y_f32;
     int32_t block_tokens;   // tokens of one pass over the codes (blockIdx.y)
-    int32_t x_cols;         // columns of the activations that shared memory holds at a time (a multiple of 256)
-    int32_t x_pitch;        // bytes between its columns (tokens, or parts of them)
+    int32_t x_pitch;        // bytes between the activations' columns (tokens, or parts of them) in shared memory
 };
+
+constexpr int kZeroLine = 1024;     // bytes of zeros that are read in place of columns that are not there
+constexpr int kColPitch = 20;      // floats between the columns of 16 sums: the four lanes of a row on different banks
+constexpr int kMaxWarps = 16;
+
+// The warp that has unit u of `units` spread over `warps` (each has [units w / warps, units (w + 1) / warps)).
+__device__ __forceinline__ int warp_of(int u, int units, int warps) { return ((u + 1) * warps - 1) / units; }
+
+// Eight activations of fp32 as bfloat16 parts: the upper half of the bits is one, and what it leaves is exact. v keeps that.
+__device__ __forceinline__ uint4 take_part(float (&v)[8]) {
+    uint32_t hi[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        hi[j] = __float_as_uint(v[j]) & 0xffff0000u;
+        v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - __uint_as_float(hi[j]);
+    }
+    return make_uint4((hi[0] >> 16) | hi[4], (hi[1] >> 16) | hi[5], (hi[2] >> 16) | hi[6], (hi[3] >> 16) | hi[7]);
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 
 // GB: 32-column blocks per scale (1, 2 or 4; wider groups repeat their scale). NT: tiles of 8 columns of activations.
 template <typename T, int NT, int GB>
-__global__ void __launch_bounds__(256) w4_product_kernel(const W4Product p) {
+__global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4Product p) {
     using M = typename Operand<T>::M;
     constexpr int PARTS = Operand<T>::parts;
-    constexpr int NS = GB == 1 ? 2 : 1;         // scales per row, stage and lane
+    constexpr int NS = 4 / GB;         // scales per row, stage and lane: the four lanes of a row hold a stage's
     extern __shared__ __align__(128) unsigned char smem[];
     const W4Quant& a = p.w;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -248,220 +282,294 @@ __global__ void __launch_bounds__(256) w4_product_kernel(const W4Product p) {
     uint32_t rank, ranks;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
-    const int tile_rows = warps * 16;
-    const int64_t row0 = (int64_t)(blockIdx.x / ranks) * tile_rows, wrow0 = row0 + warp * 16;
+    const int clusters = gridDim.x / ranks, cluster = blockIdx.x / ranks;
+    const int all_tiles = (int)((a.rows + 15) / 16), cols = (int)a.cols, all_stages = (cols + kStageCols - 1) / kStageCols;
+    const int tile0 = (int)((int64_t)all_tiles * cluster / clusters), tiles = (int)((int64_t)all_tiles * (cluster + 1) / clusters) - tile0;
+    const int st0 = (int)(all_stages * rank / ranks), stages = (int)(all_stages * (rank + 1) / ranks) - st0;
+    const int units = tiles * stages, sharing = min(warps, units);
+    const int u0 = warp < sharing ? units * warp / sharing : 0, u1 = warp < sharing ? units * (warp + 1) / sharing : 0;
     const int64_t m0 = (int64_t)blockIdx.y * p.block_tokens;
     const int mcount = (int)min((int64_t)p.block_tokens, p.tokens - m0), ncols = mcount * PARTS;
-    const int cols = (int)a.cols, all_stages = (cols + kStageCols - 1) / kStageCols;
-    const int st0 = (int)((int64_t)all_stages * rank / ranks), st1 = (int)((int64_t)all_stages * (rank + 1) / ranks);
-    const int chunk_stages = p.x_cols / kStageCols;
 
+    // Shared memory: the warps' buffers (later the CTA's sums), the activations, zeros, the sums of (tile, warp) pairs.
     const uint32_t ring = smem_u32(smem) + warp * kWarpRing;
     const uint32_t xs = smem_u32(smem) + warps * kWarpRing;
-    const uint32_t zero_line = xs + (p.block_tokens * PARTS) * p.x_pitch;    // 64 bytes of zeros, read in place of columns that are not there
-    if (threadIdx.x < 16) asm volatile("st.shared.u32 [%0], %1;" ::"r"(zero_line + threadIdx.x * 4), "r"(0));
+    const uint32_t zero_line = xs + p.block_tokens * PARTS * p.x_pitch;
+    float* const sums = reinterpret_cast<float*>(smem + warps * kWarpRing + p.block_tokens * PARTS * p.x_pitch + kZeroLine);
+    const int slot_floats = p.block_tokens * PARTS * kColPitch;
 
-    // Codes: lane l copies 16 bytes of rows l / 8, l / 8 + 4, ...; a row's eight 16-byte pieces are permuted by the row number, so
-    // that the eight rows a warp reads at a time lie on different banks.
-    const int row_bytes = (cols + 1) / 2;
-    const auto fetch = [&](int st) {
-        if (st < st1) {
-            const uint32_t dst = ring + (st & (kStages - 1)) * (16 * kStageBytes);
-            const int byte = st * kStageBytes + (lane & 7) * 16;
+    // Codes: lane l copies 16 bytes of rows l / 16, l / 16 + 2, ...; a row's 16-byte pieces are permuted by the row number, so that the
+    // eight rows a warp reads at a time lie on different banks. What lies behind the last row or column is read from the last
+    // one instead: its sums are not used, its activations are zeros.
+    const int last_byte = ((cols + 1) / 2 - 1) & ~15, my_byte = (lane & 15) * 16;
+    const uint8_t* f_base;
+    uint32_t f_off[8];
+    int f_tile = tile0 + u0 / stages, f_st = u0 % stages, fu = u0;
+    const auto fetch_rows = [&] {
+        const int64_t row = min((int64_t)f_tile * 16, a.rows - 1);
+        const int last = (int)min((int64_t)15, a.rows - 1 - row);
+        f_base = a.codes + row * a.codes_stride;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = i * 4 + (lane >> 3);
-                const bool in = wrow0 + r < a.rows && byte < row_bytes;
-                const uint8_t* src = a.codes + (in ? (wrow0 + r) * a.codes_stride + byte : 0);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + r * kStageBytes + (((lane & 7) ^ (r & 7)) << 4)), "l"(src), "r"(in ? 16 : 0) : "memory");
-            }
+        for (int i = 0; i < 8; ++i) f_off[i] = (uint32_t)min(i * 2 + (lane >> 4), last) * (uint32_t)a.codes_stride;
+    };
+    fetch_rows();
+    const auto fetch = [&] {
+        if (fu < u1) {
+            const uint32_t o = ring + (fu & (kStages - 1)) * (16 * kStageBytes) + (lane >> 4) * kStageBytes;
+            const uint8_t* const src = f_base + min((st0 + f_st) * kStageBytes + my_byte, last_byte);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(o + i * 2 * kStageBytes + (((lane & 15) ^ ((i * 2 + (lane >> 4)) & 7)) << 4)), "l"(src + f_off[i]) : "memory");
+            if (++f_st == stages) { f_st = 0; ++f_tile; fetch_rows(); }
+            ++fu;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) fetch(st0 + i);
+    fetch();
 
-    // Scales (and zero points) of a stage, one stage ahead, in registers: lane t of a row holds groups 2t and 2t + 1 (groups of
-    // 32 columns), t (64) or t & 1 (128 and wider) of the stage.
-    const int64_t ra = min(wrow0 + g, a.rows - 1) * a.groups, rb = min(wrow0 + g + 8, a.rows - 1) * a.groups;
+    // Scales (and zero points) of a stage, one stage ahead, in registers: lane t of a row holds groups t NS to t NS + NS - 1.
+    int s_tile = tile0 + u0 / stages, s_st = u0 % stages;
+    int64_t ra, rb;
+    const auto scale_rows = [&] {
+        ra = min((int64_t)s_tile * 16 + g, a.rows - 1) * a.groups;
+        rb = min((int64_t)s_tile * 16 + g + 8, a.rows - 1) * a.groups;
+    };
+    scale_rows();
     const int wide = a.group / 128;
-    float sa[NS], sb[NS], za[NS], zb[NS];
-    const auto load_scales = [&](int st, float (&sa)[NS], float (&sb)[NS], float (&za)[NS], float (&zb)[NS]) {
+    const auto load_scales = [&](float (&sa)[NS], float (&sb)[NS], float (&za)[NS], float (&zb)[NS]) {
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            int gi = GB == 1 ? st * 8 + 2 * t + i : GB == 2 ? st * 4 + t : (st * 2 + (t & 1)) / wide;
-            const bool in = gi < a.groups && st < st1;
+            int gi = (st0 + s_st) * (4 * NS) + t * NS + i;
+            if (GB == 4 && wide > 1) gi /= wide;
+            const bool in = gi < a.groups;
             gi = in ? gi : 0;
-            sa[i] = in ? load_f32(a.scales, p.scale_dtype, ra + gi) : 0.0f;
-            sb[i] = in ? load_f32(a.scales, p.scale_dtype, rb + gi) : 0.0f;
-            za[i] = a.zeros ? (float)a.zeros[ra + gi] : 8.0f;
-            zb[i] = a.zeros ? (float)a.zeros[rb + gi] : 8.0f;
+            if (p.scale_dtype == 0) {
+                sa[i] = __ldg(static_cast<const float*>(a.scales) + ra + gi);
+                sb[i] = __ldg(static_cast<const float*>(a.scales) + rb + gi);
+            } else {
+                const uint32_t ha = __ldg(static_cast<const unsigned short*>(a.scales) + ra + gi), hb = __ldg(static_cast<const unsigned short*>(a.scales) + rb + gi);
+                sa[i] = p.scale_dtype == 1 ? __uint_as_float(ha << 16) : unpack_pair<__half>(ha).x;
+                sb[i] = p.scale_dtype == 1 ? __uint_as_float(hb << 16) : unpack_pair<__half>(hb).x;
+            }
+            if (!in) sa[i] = sb[i] = 0.0f;
+            if (a.zeros) { za[i] = (float)__ldg(a.zeros + ra + gi); zb[i] = (float)__ldg(a.zeros + rb + gi); }
         }
+        if (++s_st == stages) { s_st = 0; ++s_tile; scale_rows(); }
     };
-    load_scales(st0, sa, sb, za, zb);
 
-    float acc[NT][4];
+    // The activations of this CTA's columns, eight at a time; several loads of a thread are under way at once.
+    for (int i = threadIdx.x; i < kZeroLine / 16; i += blockDim.x) sts128(zero_line + i * 16, make_uint4(0, 0, 0, 0));
+    {
+        constexpr int BATCH = PARTS == 1 ? 4 : 2;
+        // The CTAs start at different places, so that they do not all ask the same part of the L2 cache at a time.
+        const int eights = stages * (kStageCols / 8), total = eights * mcount, shift = (int)((int64_t)total * cluster / clusters);
+        for (int i0 = threadIdx.x; i0 < total; i0 += BATCH * blockDim.x) {
+            float v[BATCH][8];
+            uint32_t addr[BATCH];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
-
-    for (int c0 = st0; c0 < st1; c0 += chunk_stages) {
-        const int c1 = min(c0 + chunk_stages, st1);
-        // Activations of the columns [c0, c1) * 256, eight at a time, in the order of the codes' pairs.
-        if (c0 != st0) __syncthreads();
-        const int eights = (c1 - c0) * (kStageCols / 8);
-        for (int i = threadIdx.x; i < eights * mcount; i += blockDim.x) {
-            const int m = i / eights, e = i - m * eights, k = c0 * kStageCols + e * 8;
-            const T* row = static_cast<const T*>(a.w) + (m0 + m) * a.w_stride;
-            float v[8];
-            if (k < cols) load8(row, k, cols, a.vec, v);
-            else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-            }
-            uint32_t addr = xs + (m * PARTS) * p.x_pitch + e * 16;
-#pragma unroll
-            for (int part = 0; part < PARTS; ++part) {
-                uint32_t o[4];
-                if constexpr (PARTS == 1) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[j] = pack_pair<M>(v[j], v[j + 4]);
+            for (int j = 0; j < BATCH; ++j) {
+                const int n = i0 + j * (int)blockDim.x, i = n + shift < total ? n + shift : n + shift - total;
+                const int m = mcount > 1 ? i / eights : 0, e = i - m * eights, k = st0 * kStageCols + e * 8;
+                addr[j] = xs + m * PARTS * p.x_pitch + e * 16;
+                if (n < total && k < cols) {
+                    load8(static_cast<const T*>(a.w) + (m0 + m) * a.w_stride, k, cols, a.vec, v[j]);
                 } else {
-                    uint32_t hi[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {      // the upper half of the bits is a bfloat16; what is left is exact
-                        hi[j] = __float_as_uint(v[j]) & 0xffff0000u;
-                        v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - __uint_as_float(hi[j]);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[j] = (hi[j] >> 16) | hi[j + 4];
+                    for (int q = 0; q < 8; ++q) v[j][q] = 0.0f;
                 }
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-                addr += p.x_pitch;
+            }
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                if (i0 + j * (int)blockDim.x >= total) break;
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) {
+                    uint4 o;
+                    if constexpr (PARTS == 1) o = make_uint4(pack_pair<M>(v[j][0], v[j][4]), pack_pair<M>(v[j][1], v[j][5]), pack_pair<M>(v[j][2], v[j][6]), pack_pair<M>(v[j][3], v[j][7]));
+                    else o = take_part(v[j]);
+                    sts128(addr[j] + part * p.x_pitch, o);
+                }
             }
         }
-        __syncthreads();
+    }
+    float sa[NS], sb[NS], za[NS], zb[NS];
+    if (u0 < u1) load_scales(sa, sb, za, zb);
+    __syncthreads();
 
-        uint32_t xaddr[NT], xstep[NT];
+    uint32_t xcol[NT], xstep[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const bool in = n * 8 + g < ncols;
-            xaddr[n] = (in ? xs + (n * 8 + g) * p.x_pitch : zero_line) + t * 16;
-            xstep[n] = in ? 64 : 0;
-        }
-        for (int st = c0; st < c1; ++st) {
-            fetch(st + kStages - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-            __syncwarp();
-            float nsa[NS], nsb[NS], nza[NS], nzb[NS];
-            load_scales(st + 1, nsa, nsb, nza, nzb);
-            const uint32_t codes = ring + (st & (kStages - 1)) * (16 * kStageBytes) + g * kStageBytes + t * 4;
-            float part[NT][4];
-            float s0 = 0.0f, s1 = 0.0f;
-            uint32_t z0 = 0, z0x = 0, z1 = 0, z1x = 0;
+    for (int n = 0; n < NT; ++n) {
+        const bool in = n * 8 + g < ncols;
+        xcol[n] = (in ? xs + (n * 8 + g) * p.x_pitch : zero_line) + t * 16;
+        xstep[n] = in ? kStageCols * 2 : 0;
+    }
+    float2 acc[NT][2];      // rows g and g + 8, columns 2t and 2t + 1
 #pragma unroll
-            for (int b = 0; b < 8; ++b) {
-                if (b % GB == 0) {        // a new group
-                    const int src = (lane & ~3) | (GB == 1 ? b >> 1 : b / GB);
-                    const int i = GB == 1 ? b & 1 : 0;
-                    s0 = __shfl_sync(0xffffffffu, sa[i], src);
-                    s1 = __shfl_sync(0xffffffffu, sb[i], src);
-                    if (a.zeros || b == 0) {
-                        Codes<M>::zero_operand(a.zeros ? __shfl_sync(0xffffffffu, za[i], src) : 8.0f, z0, z0x);
-                        Codes<M>::zero_operand(a.zeros ? __shfl_sync(0xffffffffu, zb[i], src) : 8.0f, z1, z1x);
-                    }
+    for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = splat(0.0f);
+    uint32_t z0 = 0, z0x = 0, z1 = 0, z1x = 0;
+    Codes<M>::zero_operand(8.0f, z0, z0x);
+    z1 = z0; z1x = z0x;
+    int tile = u0 / stages, st = u0 % stages;
+    for (int u = u0; u < u1; ++u) {
+        fetch();
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        __syncwarp();
+        float nsa[NS] = {}, nsb[NS] = {}, nza[NS] = {}, nzb[NS] = {};
+        if (u + 1 < u1) load_scales(nsa, nsb, nza, nzb);
+        const uint32_t codes = ring + (u & (kStages - 1)) * (16 * kStageBytes) + g * kStageBytes + (g << 4) + t * 4;
+        uint32_t xa[NT];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
+        for (int n = 0; n < NT; ++n) xa[n] = xcol[n] + st * xstep[n];
+        float part[NT][4];
+        float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+        for (int b = 0; b < kStageCols / 32; ++b) {
+            if (b % GB == 0) {        // a new group
+                const int from = (lane & ~3) | (b / 4), i = (b / GB) % NS;
+                s0 = __shfl_sync(0xffffffffu, sa[i], from);
+                s1 = __shfl_sync(0xffffffffu, sb[i], from);
+                if (a.zeros) {
+                    Codes<M>::zero_operand(__shfl_sync(0xffffffffu, za[i], from), z0, z0x);
+                    Codes<M>::zero_operand(__shfl_sync(0xffffffffu, zb[i], from), z1, z1x);
                 }
-                uint32_t qa[4], qb[4];
-                Codes<M>::expand(lds32(codes + ((b ^ g) << 4)), z0, z0x, qa);
-                Codes<M>::expand(lds32(codes + 8 * kStageBytes + ((b ^ g) << 4)), z1, z1x, qb);
-                const uint32_t a0[4] = {qa[0], qb[0], qa[1], qb[1]}, a1[4] = {qa[2], qb[2], qa[3], qb[3]};
+            }
+            uint32_t qa[4], qb[4];
+            Codes<M>::expand(lds32(codes ^ (b << 4)), z0, z0x, qa);
+            Codes<M>::expand(lds32((codes ^ (b << 4)) + 8 * kStageBytes), z1, z1x, qb);
+            const uint32_t a0[4] = {qa[0], qb[0], qa[1], qb[1]}, a1[4] = {qa[2], qb[2], qa[3], qb[3]};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const uint4 x = lds128(xa[n] + b * 64);
+                if (b % GB == 0) Codes<M>::mma0(part[n], a0, x.x, x.y);
+                else Codes<M>::mma(part[n], a0, x.x, x.y);
+                Codes<M>::mma(part[n], a1, x.z, x.w);
+            }
+            if (b % GB == GB - 1) {
+                const float2 s00 = splat(s0), s11 = splat(s1);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const uint4 x = lds128(xaddr[n]);
-                    xaddr[n] += xstep[n];
-                    Codes<M>::mma(part[n], a0, x.x, x.y);
-                    Codes<M>::mma(part[n], a1, x.z, x.w);
-                }
-                if (b % GB == GB - 1) {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        acc[n][0] = __fmaf_rn(s0, part[n][0], acc[n][0]);
-                        acc[n][1] = __fmaf_rn(s0, part[n][1], acc[n][1]);
-                        acc[n][2] = __fmaf_rn(s1, part[n][2], acc[n][2]);
-                        acc[n][3] = __fmaf_rn(s1, part[n][3], acc[n][3]);
-                    }
+                    acc[n][0] = fma2_rn(s00, make_float2(part[n][0], part[n][1]), acc[n][0]);
+                    acc[n][1] = fma2_rn(s11, make_float2(part[n][2], part[n][3]), acc[n][1]);
                 }
             }
+        }
 #pragma unroll
-            for (int i = 0; i < NS; ++i) { sa[i] = nsa[i]; sb[i] = nsb[i]; za[i] = nza[i]; zb[i] = nzb[i]; }
-            __syncwarp();       // the stage may be overwritten
+        for (int i = 0; i < NS; ++i) { sa[i] = nsa[i]; sb[i] = nsb[i]; za[i] = nza[i]; zb[i] = nzb[i]; }
+        __syncwarp();       // the stage may be overwritten
+        if (++st == stages || u + 1 == u1) {     // (tile, warp) pairs come in order, each raising one of the two: tile + warp numbers them
+            float* const out = sums + (tile + warp) * slot_floats + g;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int col = n * 8 + 2 * t;
+                if (col < ncols) { out[col * kColPitch] = acc[n][0].x; out[col * kColPitch + 8] = acc[n][1].x; }
+                if (col + 1 < ncols) { out[(col + 1) * kColPitch] = acc[n][0].y; out[(col + 1) * kColPitch + 8] = acc[n][1].y; }
+                acc[n][0] = acc[n][1] = splat(0.0f);
+            }
+            st = 0;
+            ++tile;
         }
     }
 
-    // Sums of this CTA, [column][row], into the rings' place; then every rank adds its share of the rows over all ranks.
+    // The CTA's sums over the warps that had a part of a tile (and over the parts of fp32 activations), to where the buffers were:
+    // [token][row]. Then every rank adds its share of the rows over the ranks.
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    float* const red = reinterpret_cast<float*>(smem);
-    const int rpitch = tile_rows + 4;
+    float* const total = reinterpret_cast<float*>(smem);
+    const int rows_here = tiles * 16;
+    int* const shares = reinterpret_cast<int*>(total + rows_here * mcount);     // a tile's first warp, and how many
+    for (int tl = threadIdx.x; tl < tiles; tl += blockDim.x) {
+        const int w0 = warp_of(tl * stages, units, sharing);
+        shares[tl] = w0 | (warp_of(tl * stages + stages - 1, units, sharing) - w0 + 1) << 16;
+    }
+    __syncthreads();
+    for (int m = threadIdx.x / rows_here, r = threadIdx.x - m * rows_here; m < mcount;) {
+        const int w = shares[r >> 4];
+        const float* at = sums + ((r >> 4) + (w & 0xffff)) * slot_floats + m * PARTS * kColPitch + (r & 15);
+        float v = 0.0f;
+        for (int n = w >> 16; n > 0; --n, at += slot_floats) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int col = n * 8 + 2 * t + (i & 1);
-            if (col < ncols) red[col * rpitch + warp * 16 + g + (i >> 1) * 8] = acc[n][i];
+            for (int part = 0; part < PARTS; ++part) v += at[part * kColPitch];
         }
+        total[m * rows_here + r] = v;
+        for (r += blockDim.x; r >= rows_here; r -= rows_here) ++m;
     }
     if (ranks > 1) asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
     else __syncthreads();
-    const int share = tile_rows / (int)ranks, r_lo = (int)rank * share;
+    const int r_lo = rows_here * (int)rank / (int)ranks, share = rows_here * ((int)rank + 1) / (int)ranks - r_lo;
     for (int i = threadIdx.x; i < share * mcount; i += blockDim.x) {
         const int m = i / share, r = r_lo + i - m * share;
-        if (row0 + r >= a.rows) continue;
-        float v = 0.0f;
-        for (uint32_t k = 0; k < ranks; ++k)
+        const int64_t row = (int64_t)tile0 * 16 + r;
+        if (row >= a.rows) continue;
+        const float* const at = total + m * rows_here + r;
+        float v;
+        if (ranks > 1) {
+            float of[8];
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) {
-                const float* at = red + (m * PARTS + part) * rpitch + r;
-                v += ranks > 1 ? ld_rank(smem_u32(at), k) : *at;
-            }
-        if (p.bias) v += p.bias[row0 + r];
-        const int64_t o = (m0 + m) * p.y_stride + row0 + r;
+            for (uint32_t k = 0; k < 8; ++k) of[k] = k < ranks ? ld_rank(smem_u32(at), k) : 0.0f;
+            v = of[0];
+#pragma unroll
+            for (int k = 1; k < 8; ++k) v += of[k];
+        } else {
+            v = *at;
+        }
+        v *= 1.0f / Codes<M>::unit;
+        if (p.bias) v += p.bias[row];
+        const int64_t o = (m0 + m) * p.y_stride + row;
         if (p.y_f32) static_cast<float*>(p.y)[o] = v;
         else static_cast<T*>(p.y)[o] = from_f32<T>(v);
     }
     if (ranks > 1) asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
+// How a product is laid out: CTAs per cluster, clusters, warps per CTA, shared memory.
+struct ProductPlan {
+    int ranks, clusters, warps;
+    size_t bytes;
+    int64_t cost;
+};
+
+// The layout with the fewest stages per CTA (as its busiest warp has them) among those that fit, and a little for each cluster's
+// last exchange. Clusters of 1, 2, 4 and 8 that run side by side
+// at one CTA per SM: 148, 74, 33 and 15 on this part.
+ProductPlan plan_product(int64_t rows, int64_t cols, int columns, int64_t blocks) {
+    const int side_by_side[4] = {148, 74, 33, 15};
+    const int64_t tiles = (rows + 15) / 16, stages = (cols + kStageCols - 1) / kStageCols;
+    ProductPlan best = {0, 0, 0, 0, INT64_MAX};
+    for (int i = 0; i < 4; ++i) {
+        const int ranks = 1 << i;
+        if (ranks > stages && i) break;
+        const int64_t ns = (stages + ranks - 1) / ranks;
+        for (int warps = kMaxWarps; warps >= 8; warps -= 8) {
+            const int64_t fixed = (int64_t)warps * kWarpRing + columns * (ns * kStageCols * 2 + kXPad) + kZeroLine, slot = (int64_t)columns * kColPitch * 4;
+            // tiles whose sums fit, by warp behind the rest and by CTA into the buffers
+            const int64_t room = std::min((227 * 1024 - 1024 - fixed) / slot - warps, (int64_t)warps * kWarpRing / (columns * 64 + 4));
+            if (fixed > 226 * 1024 || room < 1) continue;
+            const int64_t at_a_time = std::max<int64_t>(1, side_by_side[i] / blocks);
+            const int64_t per = std::min((tiles + at_a_time - 1) / at_a_time, room), clusters = (tiles + per - 1) / per;
+            const int64_t waves = (clusters * blocks + side_by_side[i] - 1) / side_by_side[i];
+            const int64_t cost = waves * (2 * warps * ((per * ns + warps - 1) / warps) + 16 + 8 * i);
+            if (cost < best.cost) best = {ranks, (int)clusters, warps, (size_t)(fixed + (per + warps) * slot), cost};
+            break;
+        }
+    }
+    return best;
+}
+
 template <typename T, int NT, int GB>
-cudaError_t launch_product(W4Product p, cudaStream_t s) {
-    constexpr int PARTS = Operand<T>::parts;
-    const int warps = 8, tile_rows = warps * 16;
-    const int64_t tiles = (p.w.rows + tile_rows - 1) / tile_rows, blocks = (p.tokens + p.block_tokens - 1) / p.block_tokens;
-    const int stages = (int)((p.w.cols + kStageCols - 1) / kStageCols);
-    int ranks = 1;
-    while (ranks < 8 && tiles * blocks * ranks < 148 * 2 && stages >= ranks * 4) ranks *= 2;
-    const int range = (stages + ranks - 1) / ranks, columns = p.block_tokens * PARTS;
-    const int limit = NT <= 2 ? 40 * 1024 : 64 * 1024;
-    int chunk = range;
-    while (chunk > 1 && (int64_t)columns * (chunk * kStageCols * 2 + kXPad) > limit) chunk = (chunk + 1) / 2;
-    p.x_cols = chunk * kStageCols;
-    p.x_pitch = p.x_cols * 2 + kXPad;
-    const size_t bytes = std::max((size_t)warps * kWarpRing + (size_t)columns * p.x_pitch + 64, (size_t)columns * (tile_rows + 4) * 4);
+cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t blocks, cudaStream_t s) {
     auto kernel = w4_product_kernel<T, NT, GB>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.bytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * ranks), (unsigned)blocks);
-    cfg.blockDim = dim3(warps * 32);
-    cfg.dynamicSmemBytes = bytes;
+    cfg.gridDim = dim3((unsigned)(plan.clusters * plan.ranks), (unsigned)blocks);
+    cfg.blockDim = dim3(plan.warps * 32);
+    cfg.dynamicSmemBytes = plan.bytes;
     cfg.stream = s;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = ranks;
+    attr.val.clusterDim.x = plan.ranks;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
-    cfg.numAttrs = ranks > 1 ? 1 : 0;
+    cfg.numAttrs = plan.ranks > 1 ? 1 : 0;
     e = cudaLaunchKernelEx(&cfg, kernel, p);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -505,26 +613,37 @@ cudaError_t launch_w4_matvec(const W4Matrix& m, const void* x, int x_dtype, int6
         p.tokens = tokens; p.bias = bias; p.y = y; p.y_stride = y_stride;
         p.scale_dtype = m.scale_dtype;
         p.y_f32 = y_dtype == 0;
-        const int64_t columns = tokens * PARTS;
+        // Up to 32 columns of activations at a time (a token is PARTS of them), as few as fit beside the rings.
+        int64_t block = std::min<int64_t>(tokens, 32 / PARTS), blocks;
+        ProductPlan plan;
+        for (;; block = (block + 1) / 2) {
+            blocks = std::min<int64_t>((tokens + block - 1) / block, 65535);
+            plan = plan_product(m.rows, m.cols, (int)block * PARTS, blocks);
+            if (plan.ranks || block == 1) break;
+        }
+        if (!plan.ranks) return cudaErrorInvalidConfiguration;      // cannot be: see LPMM_W4_MAX_COLS
+        block = std::min(block, (tokens + blocks - 1) / blocks);    // even blocks
+        p.block_tokens = (int)block;
+        const int64_t ns = ((m.cols + kStageCols - 1) / kStageCols + plan.ranks - 1) / plan.ranks;
+        p.x_pitch = (int)(ns * kStageCols * 2 + kXPad);
         const auto run = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
-            p.block_tokens = (int)std::min<int64_t>(tokens, NT * 8 / PARTS);
             // grid.y counts blocks of tokens and ends at 65535; the rest is another launch's
-            const int64_t most = (int64_t)65535 * p.block_tokens;
-            for (int64_t done = 0; done < tokens; done += most) {
+            for (int64_t done = 0; done < tokens; done += blocks * block) {
                 W4Product q = p;
-                q.tokens = std::min(most, tokens - done);
+                q.tokens = std::min(blocks * block, tokens - done);
                 q.w.w = static_cast<const T*>(x) + done * x_stride;
                 q.y = static_cast<char*>(y) + done * y_stride * (p.y_f32 ? 4 : (int64_t)sizeof(T));
-                const cudaError_t e = m.group == 32 ? launch_product<T, NT, 1>(q, s) : m.group == 64 ? launch_product<T, NT, 2>(q, s) : launch_product<T, NT, 4>(q, s);
+                const int64_t nb = (q.tokens + block - 1) / block;
+                const cudaError_t e = m.group == 32 ? launch_product<T, NT, 1>(q, plan, nb, s) : m.group == 64 ? launch_product<T, NT, 2>(q, plan, nb, s) : launch_product<T, NT, 4>(q, plan, nb, s);
                 if (e != cudaSuccess) return e;
             }
             return cudaSuccess;
         };
+        const int64_t columns = block * PARTS;
         if (columns <= 8) return run(std::integral_constant<int, 1>{});
         if (columns <= 16) return run(std::integral_constant<int, 2>{});
-        if (columns <= 32) return run(std::integral_constant<int, 4>{});
-        return run(std::integral_constant<int, 8>{});
+        return run(std::integral_constant<int, 4>{});
     });
 }
 
