@@ -246,6 +246,9 @@ struct W4Product {
     int32_t scale_dtype, y_f32;
     int32_t block_tokens;   // tokens of one pass over the codes (blockIdx.y)
     int32_t x_pitch;        // bytes between the activations' columns (tokens, or parts of them) in shared memory
+    int32_t tiles, tiles_extra;   // tiles of 16 rows per cluster; the first tiles_extra clusters have one more
+    int32_t log_ranks, log_warps;
+    int32_t log_run;        // threads that take a token's activations while they are put into shared memory (a power of two)
 };
 
 constexpr int kZeroLine = 1024;     // bytes of zeros that are read in place of columns that are not there
@@ -269,6 +272,17 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+// Eight consecutive 16-bit elements of a row from column c on, as they are; zeros behind the row's end.
+template <typename T>
+__device__ __forceinline__ uint4 load8_bits(const T* row, int c, int cols, bool vec) {
+    if (vec && c + 8 <= cols) return __ldg(reinterpret_cast<const uint4*>(row + c));
+    const unsigned short* const u = reinterpret_cast<const unsigned short*>(row);
+    uint32_t v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? __ldg(u + c + i) : 0u;
+    return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
 // GB: 32-column blocks per scale (1, 2 or 4; wider groups repeat their scale). NT: tiles of 8 columns of activations.
 template <typename T, int NT, int GB>
 __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4Product p) {
@@ -279,15 +293,13 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     const W4Quant& a = p.w;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int g = lane >> 2, t = lane & 3;
-    uint32_t rank, ranks;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
-    const int clusters = gridDim.x / ranks, cluster = blockIdx.x / ranks;
-    const int all_tiles = (int)((a.rows + 15) / 16), cols = (int)a.cols, all_stages = (cols + kStageCols - 1) / kStageCols;
-    const int tile0 = (int)((int64_t)all_tiles * cluster / clusters), tiles = (int)((int64_t)all_tiles * (cluster + 1) / clusters) - tile0;
-    const int st0 = (int)(all_stages * rank / ranks), stages = (int)(all_stages * (rank + 1) / ranks) - st0;
-    const int units = tiles * stages, sharing = min(warps, units);
-    const int u0 = warp < sharing ? units * warp / sharing : 0, u1 = warp < sharing ? units * (warp + 1) / sharing : 0;
+    const int ranks = 1 << p.log_ranks, rank = blockIdx.x & (ranks - 1), cluster = blockIdx.x >> p.log_ranks;
+    const int cols = (int)a.cols, all_stages = (cols + kStageCols - 1) / kStageCols;
+    const int tiles = p.tiles + (cluster < p.tiles_extra), tile0 = cluster * p.tiles + min(cluster, p.tiles_extra);
+    const int st0 = all_stages * rank >> p.log_ranks, stages = (all_stages * (rank + 1) >> p.log_ranks) - st0;
+    const int units = tiles * stages, sharing = min(warps, units);      // each warp's share, [u0, u1)
+    const int u0 = units > warps ? units * warp >> p.log_warps : min(warp, units), u1 = units > warps ? units * (warp + 1) >> p.log_warps : min(warp + 1, units);
+    const int first_tile = u0 / stages, first_stage = u0 - first_tile * stages;
     const int64_t m0 = (int64_t)blockIdx.y * p.block_tokens;
     const int mcount = (int)min((int64_t)p.block_tokens, p.tokens - m0), ncols = mcount * PARTS;
 
@@ -304,7 +316,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     const int last_byte = ((cols + 1) / 2 - 1) & ~15, my_byte = (lane & 15) * 16;
     const uint8_t* f_base;
     uint32_t f_off[8];
-    int f_tile = tile0 + u0 / stages, f_st = u0 % stages, fu = u0;
+    int f_tile = tile0 + first_tile, f_st = first_stage, fu = u0;
     const auto fetch_rows = [&] {
         const int64_t row = min((int64_t)f_tile * 16, a.rows - 1);
         const int last = (int)min((int64_t)15, a.rows - 1 - row);
@@ -328,7 +340,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     fetch();
 
     // Scales (and zero points) of a stage, one stage ahead, in registers: lane t of a row holds groups t NS to t NS + NS - 1.
-    int s_tile = tile0 + u0 / stages, s_st = u0 % stages;
+    int s_tile = tile0 + first_tile, s_st = first_stage;
     int64_t ra, rb;
     const auto scale_rows = [&] {
         ra = min((int64_t)s_tile * 16 + g, a.rows - 1) * a.groups;
@@ -357,36 +369,39 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
         if (++s_st == stages) { s_st = 0; ++s_tile; scale_rows(); }
     };
 
-    // The activations of this CTA's columns, eight at a time; several loads of a thread are under way at once.
+    // The activations of this CTA's columns, eight at a time: 2^log_run threads side by side take a token's, several tokens' loads
+    // are under way at once, and the clusters start at different places, so that they do not all ask the same part of the L2
+    // cache at a time.
     for (int i = threadIdx.x; i < kZeroLine / 16; i += blockDim.x) sts128(zero_line + i * 16, make_uint4(0, 0, 0, 0));
     {
-        constexpr int BATCH = PARTS == 1 ? 4 : 2;
-        // The CTAs start at different places, so that they do not all ask the same part of the L2 cache at a time.
-        const int eights = stages * (kStageCols / 8), total = eights * mcount, shift = (int)((int64_t)total * cluster / clusters);
-        for (int i0 = threadIdx.x; i0 < total; i0 += BATCH * blockDim.x) {
-            float v[BATCH][8];
-            uint32_t addr[BATCH];
+        constexpr int BATCH = PARTS == 1 ? 8 : 4;
+        const int eights = stages * (kStageCols / 8), run = 1 << p.log_run, m_step = blockDim.x >> p.log_run, shift = (cluster * 13) % eights;
+        for (int e0 = threadIdx.x & (run - 1); e0 < eights; e0 += run) {
+            const int e = e0 + shift < eights ? e0 + shift : e0 + shift - eights, k = st0 * kStageCols + e * 8;
+            for (int mb = threadIdx.x >> p.log_run; mb < mcount; mb += BATCH * m_step) {
+                const T* src = static_cast<const T*>(a.w) + (m0 + mb) * a.w_stride;
+                const uint32_t dst = xs + mb * PARTS * p.x_pitch + e * 16;
+                if constexpr (PARTS == 1) {
+                    uint4 v[BATCH];
 #pragma unroll
-            for (int j = 0; j < BATCH; ++j) {
-                const int n = i0 + j * (int)blockDim.x, i = n + shift < total ? n + shift : n + shift - total;
-                const int m = mcount > 1 ? i / eights : 0, e = i - m * eights, k = st0 * kStageCols + e * 8;
-                addr[j] = xs + m * PARTS * p.x_pitch + e * 16;
-                if (n < total && k < cols) {
-                    load8(static_cast<const T*>(a.w) + (m0 + m) * a.w_stride, k, cols, a.vec, v[j]);
+                    for (int j = 0; j < BATCH; ++j)
+                        v[j] = mb + j * m_step < mcount ? load8_bits(src + j * m_step * a.w_stride, k, cols, a.vec) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int j = 0; j < BATCH; ++j)
+                        if (mb + j * m_step < mcount)
+                            sts128(dst + j * m_step * p.x_pitch, make_uint4(__byte_perm(v[j].x, v[j].z, 0x5410), __byte_perm(v[j].x, v[j].z, 0x7632),
+                                                                            __byte_perm(v[j].y, v[j].w, 0x5410), __byte_perm(v[j].y, v[j].w, 0x7632)));
                 } else {
+                    float v[BATCH][8];
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) v[j][q] = 0.0f;
-                }
-            }
+                    for (int j = 0; j < BATCH; ++j)
+                        if (mb + j * m_step < mcount) load8(src + j * m_step * a.w_stride, k, cols, a.vec, v[j]);
 #pragma unroll
-            for (int j = 0; j < BATCH; ++j) {
-                if (i0 + j * (int)blockDim.x >= total) break;
+                    for (int j = 0; j < BATCH; ++j) {
+                        if (mb + j * m_step >= mcount) break;
 #pragma unroll
-                for (int part = 0; part < PARTS; ++part) {
-                    uint4 o;
-                    if constexpr (PARTS == 1) o = make_uint4(pack_pair<M>(v[j][0], v[j][4]), pack_pair<M>(v[j][1], v[j][5]), pack_pair<M>(v[j][2], v[j][6]), pack_pair<M>(v[j][3], v[j][7]));
-                    else o = take_part(v[j]);
-                    sts128(addr[j] + part * p.x_pitch, o);
+                        for (int part = 0; part < PARTS; ++part) sts128(dst + (j * m_step * PARTS + part) * p.x_pitch, take_part(v[j]));
+                    }
                 }
             }
         }
@@ -408,7 +423,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     uint32_t z0 = 0, z0x = 0, z1 = 0, z1x = 0;
     Codes<M>::zero_operand(8.0f, z0, z0x);
     z1 = z0; z1x = z0x;
-    int tile = u0 / stages, st = u0 % stages;
+    int tile = first_tile, st = first_stage;
     for (int u = u0; u < u1; ++u) {
         fetch();
         asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
@@ -494,7 +509,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     }
     if (ranks > 1) asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
     else __syncthreads();
-    const int r_lo = rows_here * (int)rank / (int)ranks, share = rows_here * ((int)rank + 1) / (int)ranks - r_lo;
+    const int r_lo = rows_here * rank >> p.log_ranks, share = (rows_here * (rank + 1) >> p.log_ranks) - r_lo;
     for (int i = threadIdx.x; i < share * mcount; i += blockDim.x) {
         const int m = i / share, r = r_lo + i - m * share;
         const int64_t row = (int64_t)tile0 * 16 + r;
@@ -504,7 +519,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
         if (ranks > 1) {
             float of[8];
 #pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) of[k] = k < ranks ? ld_rank(smem_u32(at), k) : 0.0f;
+            for (int k = 0; k < 8; ++k) of[k] = k < ranks ? ld_rank(smem_u32(at), k) : 0.0f;
             v = of[0];
 #pragma unroll
             for (int k = 1; k < 8; ++k) v += of[k];
@@ -626,6 +641,12 @@ cudaError_t launch_w4_matvec(const W4Matrix& m, const void* x, int x_dtype, int6
         p.block_tokens = (int)block;
         const int64_t ns = ((m.cols + kStageCols - 1) / kStageCols + plan.ranks - 1) / plan.ranks;
         p.x_pitch = (int)(ns * kStageCols * 2 + kXPad);
+        const int64_t tiles = (m.rows + 15) / 16;
+        p.tiles = (int)(tiles / plan.clusters);
+        p.tiles_extra = (int)(tiles % plan.clusters);
+        while (1 << p.log_ranks < plan.ranks) ++p.log_ranks;
+        while (1 << p.log_warps < plan.warps) ++p.log_warps;
+        while (1 << p.log_run < ns * (kStageCols / 8) && 1 << p.log_run < plan.warps * 32) ++p.log_run;
         const auto run = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
             // grid.y counts blocks of tokens and ends at 65535; the rest is another launch's
