@@ -144,8 +144,8 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
 // (8 significant bits each), as three columns instead of one.
 //
 // One CTA per SM holds the activations in shared memory and goes through tiles of 16 rows; its warps share out the stages (16 rows
-// by 512 columns, 4 KB of codes) of all its tiles evenly, in order, each streaming its own through two buffers of its own in
-// shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. A lane reads one 32-bit word =
+// by 512 columns, 4 KB of codes) of all its tiles evenly, in order, each streaming its own through two or three buffers of its
+// own in shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. A lane reads one 32-bit word =
 // 8 codes of one row per 32 columns; the pairs that its halves hold, (0, 4), (1, 5), (2, 6), (3, 7), are brought to the tensor
 // cores' operand by a mask and one exact multiply-add. The order of the columns inside a product is free as long as both operands
 // have the same: the activations' pairs are put into that order.
@@ -154,8 +154,7 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
 // fit one CTA or the tiles are few, are added in a fixed order at the end: results are the same bits every time.
 
 constexpr int kStageCols = 512, kStageBytes = kStageCols / 2;   // columns of one stage; its bytes per row
-constexpr int kStages = 2;
-constexpr int kWarpRing = kStages * 16 * kStageBytes;           // 8 KB
+constexpr int kStage = 16 * kStageBytes;                        // 4 KB
 constexpr int kXPad = 64;                                       // bytes between columns: neighbouring columns on other banks
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -284,8 +283,11 @@ __device__ __forceinline__ uint4 load8_bits(const T* row, int c, int cols, bool 
 }
 
 // GB: 32-column blocks per scale (1, 2 or 4; wider groups repeat their scale). NT: tiles of 8 columns of activations.
-template <typename T, int NT, int GB>
-__global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4Product p) {
+// DEPTH: stages a warp holds, the one it works on among them. Wide products (NT = 4) run with 8 warps and twice the registers: 12 of
+// a group's sums and as many of a row's stay in registers beside the operands of several blocks.
+constexpr int most_warps(int nt) { return nt == 4 ? 8 : kMaxWarps; }
+template <typename T, int NT, int GB, int DEPTH>
+__global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(const W4Product p) {
     using M = typename Operand<T>::M;
     constexpr int PARTS = Operand<T>::parts;
     constexpr int NS = 4 / GB;         // scales per row, stage and lane: the four lanes of a row hold a stage's
@@ -304,10 +306,10 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     const int mcount = (int)min((int64_t)p.block_tokens, p.tokens - m0), ncols = mcount * PARTS;
 
     // Shared memory: the warps' buffers (later the CTA's sums), the activations, zeros, the sums of (tile, warp) pairs.
-    const uint32_t ring = smem_u32(smem) + warp * kWarpRing;
-    const uint32_t xs = smem_u32(smem) + warps * kWarpRing;
+    const uint32_t ring = smem_u32(smem) + warp * (DEPTH * kStage);
+    const uint32_t xs = smem_u32(smem) + warps * (DEPTH * kStage);
     const uint32_t zero_line = xs + p.block_tokens * PARTS * p.x_pitch;
-    float* const sums = reinterpret_cast<float*>(smem + warps * kWarpRing + p.block_tokens * PARTS * p.x_pitch + kZeroLine);
+    float* const sums = reinterpret_cast<float*>(smem + warps * (DEPTH * kStage) + p.block_tokens * PARTS * p.x_pitch + kZeroLine);
     const int slot_floats = p.block_tokens * PARTS * kColPitch;
 
     // Codes: lane l copies 16 bytes of rows l / 16, l / 16 + 2, ...; a row's 16-byte pieces are permuted by the row number, so that the
@@ -317,6 +319,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     const uint8_t* f_base;
     uint32_t f_off[8];
     int f_tile = tile0 + first_tile, f_st = first_stage, fu = u0;
+    uint32_t f_slot = 0;
     const auto fetch_rows = [&] {
         const int64_t row = min((int64_t)f_tile * 16, a.rows - 1);
         const int last = (int)min((int64_t)15, a.rows - 1 - row);
@@ -327,7 +330,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     fetch_rows();
     const auto fetch = [&] {
         if (fu < u1) {
-            const uint32_t o = ring + (fu & (kStages - 1)) * (16 * kStageBytes) + (lane >> 4) * kStageBytes;
+            const uint32_t o = ring + f_slot + (lane >> 4) * kStageBytes;
+            f_slot = f_slot == (DEPTH - 1) * kStage ? 0 : f_slot + kStage;
             const uint8_t* const src = f_base + min((st0 + f_st) * kStageBytes + my_byte, last_byte);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -337,7 +341,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    fetch();
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; ++i) fetch();
 
     // Scales (and zero points) of a stage, one stage ahead, in registers: lane t of a row holds groups t NS to t NS + NS - 1.
     int s_tile = tile0 + first_tile, s_st = first_stage;
@@ -424,13 +429,15 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     Codes<M>::zero_operand(8.0f, z0, z0x);
     z1 = z0; z1x = z0x;
     int tile = first_tile, st = first_stage;
+    uint32_t slot = 0;
     for (int u = u0; u < u1; ++u) {
         fetch();
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
         __syncwarp();
         float nsa[NS] = {}, nsb[NS] = {}, nza[NS] = {}, nzb[NS] = {};
         if (u + 1 < u1) load_scales(nsa, nsb, nza, nzb);
-        const uint32_t codes = ring + (u & (kStages - 1)) * (16 * kStageBytes) + g * kStageBytes + (g << 4) + t * 4;
+        const uint32_t codes = ring + slot + g * kStageBytes + (g << 4) + t * 4;
+        slot = slot == (DEPTH - 1) * kStage ? 0 : slot + kStage;
         uint32_t xa[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) xa[n] = xcol[n] + st * xstep[n];
@@ -490,22 +497,20 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     __syncthreads();
     float* const total = reinterpret_cast<float*>(smem);
     const int rows_here = tiles * 16;
-    int* const shares = reinterpret_cast<int*>(total + rows_here * mcount);     // a tile's first warp, and how many
-    for (int tl = threadIdx.x; tl < tiles; tl += blockDim.x) {
-        const int w0 = warp_of(tl * stages, units, sharing);
-        shares[tl] = w0 | (warp_of(tl * stages + stages - 1, units, sharing) - w0 + 1) << 16;
-    }
-    __syncthreads();
-    for (int m = threadIdx.x / rows_here, r = threadIdx.x - m * rows_here; m < mcount;) {
-        const int w = shares[r >> 4];
-        const float* at = sums + ((r >> 4) + (w & 0xffff)) * slot_floats + m * PARTS * kColPitch + (r & 15);
-        float v = 0.0f;
-        for (int n = w >> 16; n > 0; --n, at += slot_floats) {
+    const int half = lane >> 4;      // a warp takes a tile, two tokens at a time
+    for (int tl = warp; tl < tiles; tl += warps) {
+        const int w0 = warp_of(tl * stages, units, sharing), n = warp_of(tl * stages + stages - 1, units, sharing) - w0 + 1;
+        const float* const from = sums + (tl + w0) * slot_floats + (lane & 15);
+        float* const to = total + tl * 16 + (lane & 15);
+#pragma unroll 4
+        for (int m = half; m < mcount; m += 2) {
+            float v = 0.0f;
+            for (int i = 0; i < n; ++i) {
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) v += at[part * kColPitch];
+                for (int part = 0; part < PARTS; ++part) v += from[i * slot_floats + (m * PARTS + part) * kColPitch];
+            }
+            to[m * rows_here] = v;
         }
-        total[m * rows_here + r] = v;
-        for (r += blockDim.x; r >= rows_here; r -= rows_here) ++m;
     }
     if (ranks > 1) asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
     else __syncthreads();
@@ -535,43 +540,43 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
     if (ranks > 1) asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
-// How a product is laid out: CTAs per cluster, clusters, warps per CTA, shared memory.
+// How a product is laid out: CTAs per cluster, clusters, warps per CTA, stages that a warp holds, shared memory.
 struct ProductPlan {
-    int ranks, clusters, warps;
+    int ranks, clusters, warps, depth;
     size_t bytes;
     int64_t cost;
 };
 
 // The layout with the fewest stages per CTA (as its busiest warp has them) among those that fit, and a little for each cluster's
-// last exchange. Clusters of 1, 2, 4 and 8 that run side by side
-// at one CTA per SM: 148, 74, 33 and 15 on this part.
+// last exchange. Clusters of 1, 2, 4 and 8 that run side by side at one CTA per SM: 148, 74, 33 and 15 on this part. A third
+// stage per warp, where it fits, keeps more of HBM's latency covered (32000 x 4096, one token: 22.5 us with two stages).
 ProductPlan plan_product(int64_t rows, int64_t cols, int columns, int64_t blocks) {
     const int side_by_side[4] = {148, 74, 33, 15};
-    const int64_t tiles = (rows + 15) / 16, stages = (cols + kStageCols - 1) / kStageCols;
-    ProductPlan best = {0, 0, 0, 0, INT64_MAX};
+    const int64_t tiles = (rows + 15) / 16, stages = (cols + kStageCols - 1) / kStageCols, room = 227 * 1024 - 1024;
+    const int warps = columns > 16 ? 8 : kMaxWarps;
+    ProductPlan best = {0, 0, 0, 0, 0, INT64_MAX};
     for (int i = 0; i < 4; ++i) {
         const int ranks = 1 << i;
         if (ranks > stages && i) break;
-        const int64_t ns = (stages + ranks - 1) / ranks;
-        for (int warps = kMaxWarps; warps >= 8; warps -= 8) {
-            const int64_t fixed = (int64_t)warps * kWarpRing + columns * (ns * kStageCols * 2 + kXPad) + kZeroLine, slot = (int64_t)columns * kColPitch * 4;
+        const int64_t ns = (stages + ranks - 1) / ranks, slot = (int64_t)columns * kColPitch * 4;
+        for (int depth = 3; depth >= 2; --depth) {
+            const int64_t ring = (int64_t)warps * depth * kStage, fixed = ring + columns * (ns * kStageCols * 2 + kXPad) + kZeroLine;
             // tiles whose sums fit, by warp behind the rest and by CTA into the buffers
-            const int64_t room = std::min((227 * 1024 - 1024 - fixed) / slot - warps, (int64_t)warps * kWarpRing / (columns * 64 + 4));
-            if (fixed > 226 * 1024 || room < 1) continue;
+            const int64_t fit = std::min((room - fixed) / slot - warps, ring / (columns * 64));
+            if (fixed > room || fit < 1) continue;
             const int64_t at_a_time = std::max<int64_t>(1, side_by_side[i] / blocks);
-            const int64_t per = std::min((tiles + at_a_time - 1) / at_a_time, room), clusters = (tiles + per - 1) / per;
+            const int64_t per = std::min((tiles + at_a_time - 1) / at_a_time, fit), clusters = (tiles + per - 1) / per;
             const int64_t waves = (clusters * blocks + side_by_side[i] - 1) / side_by_side[i];
             const int64_t cost = waves * (2 * warps * ((per * ns + warps - 1) / warps) + 16 + 8 * i);
-            if (cost < best.cost) best = {ranks, (int)clusters, warps, (size_t)(fixed + (per + warps) * slot), cost};
-            break;
+            if (cost < best.cost) best = {ranks, (int)clusters, warps, depth, (size_t)(fixed + (per + warps) * slot), cost};
         }
     }
     return best;
 }
 
-template <typename T, int NT, int GB>
+template <typename T, int NT, int GB, int DEPTH>
 cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t blocks, cudaStream_t s) {
-    auto kernel = w4_product_kernel<T, NT, GB>;
+    auto kernel = w4_product_kernel<T, NT, GB, DEPTH>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.bytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -587,6 +592,11 @@ cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t 
     cfg.numAttrs = plan.ranks > 1 ? 1 : 0;
     e = cudaLaunchKernelEx(&cfg, kernel, p);
     return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+template <typename T, int NT, int GB>
+cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t blocks, cudaStream_t s) {
+    return plan.depth == 3 ? launch_product<T, NT, GB, 3>(p, plan, blocks, s) : launch_product<T, NT, GB, 2>(p, plan, blocks, s);
 }
 
 W4Quant pack_args(const W4Matrix& m, const void* w, int64_t stride, int es) {

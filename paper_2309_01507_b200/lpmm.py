@@ -466,33 +466,32 @@ DISTILL_MAX_TOP, DISTILL_MAX_VOCAB = 1024, 262144
 _DTYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 
-class _Enqueue:
-    """Where a call's work goes: the caller's stream (its raw pointer is `ptr`) or the current one of `device`. Results that
-    are allocated inside the block belong to that stream, and tensors handed to use() stay alive until its work is done, also
-    when they were made on another stream. Ordering that stream behind the tensors' producers is the caller's part."""
+class _elsewhere:
+    """For calls whose work does not go to the current stream of the current device: makes `stream` (or the current stream of
+    `device`) the current one, so that results belong to it, and keeps the tensors given alive until its work is done, also when
+    they were made on another stream. Ordering that stream behind the tensors' producers is the caller's part."""
 
-    def __init__(self, stream, device):
-        self.stream, self.guards = stream, ()
+    def __init__(self, stream, device, *tensors):
+        self.guard = torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
         if stream is not None:
-            self.guards = (torch.cuda.stream(stream),)          # makes the stream's device current too
-        elif device.index != torch.cuda.current_device():
-            self.guards = (torch.cuda.device(device),)
-
-    def __enter__(self):
-        for g in self.guards:
-            g.__enter__()
-        self.ptr = (self.stream or torch.cuda.current_stream()).cuda_stream
-        return self
-
-    def __exit__(self, *exc):
-        for g in self.guards:
-            g.__exit__(*exc)
-
-    def use(self, *tensors):
-        if self.stream is not None:
             for t in tensors:
                 if t is not None:
-                    t.record_stream(self.stream)
+                    t.record_stream(stream)
+
+    def __enter__(self):
+        self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        self.guard.__exit__(*exc)
+
+
+def _here(stream, device) -> bool:
+    return stream is None and device.index == torch.cuda.current_device()
+
+
+def _raw_stream(device) -> int:
+    """The current stream's pointer, without a Stream object around it (3 us a call)."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _need(ok: bool, message: str) -> None:
@@ -503,9 +502,13 @@ def _need(ok: bool, message: str) -> None:
 def _rows_of(x: torch.Tensor, name: str) -> int:
     """Distance between the rows of a matrix whose rows are contiguous."""
     rows, cols = x.shape
-    _need(cols <= 1 or x.stride(1) == 1, f"the rows of {name} must be contiguous")
-    stride = x.stride(0) if rows > 1 else max(x.stride(0), cols)
-    _need(stride >= cols, f"the rows of {name} must not overlap")
+    stride, step = x.stride()
+    if cols > 1 and step != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    if stride < cols:
+        if rows > 1:
+            raise ValueError(f"the rows of {name} must not overlap")
+        return cols
     return stride
 
 
@@ -537,6 +540,7 @@ class W4Matrix:
         self._c = W4(codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), rows, cols, stride, group,
                      _dtype_of(scales, "scales"))
         self._ref = C.byref(self._c)
+        self.device = codes.device
 
     @property
     def shape(self):
@@ -546,85 +550,109 @@ class W4Matrix:
 def w4_quantize(w: torch.Tensor, *, group: int = 128, zero_points: bool = False, scale_dtype=torch.float32, stream=None) -> W4Matrix:
     """lpmm_w4_quantize: the 4-bit form of a matrix (float32, bfloat16 or float16, rows contiguous)."""
     _need(w.is_cuda and w.dim() == 2 and w.numel() > 0, "w must be a non-empty 2-D CUDA tensor")
+    if not _here(stream, w.device):
+        with _elsewhere(stream, w.device, w):
+            return w4_quantize(w, group=group, zero_points=zero_points, scale_dtype=scale_dtype)
     _need(group > 0 and scale_dtype in _DTYPE, "group must be positive and scale_dtype float32, bfloat16 or float16")
     dtype, stride = _dtype_of(w, "w"), _rows_of(w, "w")
     rows, cols = w.shape
     groups = -(-cols // group)
-    with _Enqueue(stream, w.device) as q:
-        codes = torch.empty(rows, -(-cols // 32) * 16, dtype=torch.uint8, device=w.device)
-        scales = torch.empty(rows, groups, dtype=scale_dtype, device=w.device)
-        zeros = torch.empty(rows, groups, dtype=torch.uint8, device=w.device) if zero_points else None
-        m = W4Matrix(codes, scales, cols, group=group, zeros=zeros)
-        q.use(w)
-        _check(lib().lpmm_w4_quantize(w.data_ptr(), dtype, stride, m._ref, q.ptr), "lpmm_w4_quantize")
+    codes = w.new_empty((rows, -(-cols // 32) * 16), dtype=torch.uint8)
+    scales = w.new_empty((rows, groups), dtype=scale_dtype)
+    zeros = w.new_empty((rows, groups), dtype=torch.uint8) if zero_points else None
+    m = W4Matrix(codes, scales, cols, group=group, zeros=zeros)
+    _check(lib().lpmm_w4_quantize(w.data_ptr(), dtype, stride, m._ref, _raw_stream(w.device)), "lpmm_w4_quantize")
     return m
 
 
 def w4_dequantize(m: W4Matrix, dtype=torch.float32, *, out=None, stream=None) -> torch.Tensor:
     """lpmm_w4_dequantize: the matrix the codes stand for, in `dtype` (or into `out`, whose type then counts)."""
-    with _Enqueue(stream, m.codes.device) as q:
-        if out is None:
-            _need(dtype in _DTYPE, "dtype must be float32, bfloat16 or float16")
-            out = torch.empty(m.rows, m.cols, dtype=dtype, device=m.codes.device)
-        else:
-            _need(out.shape == m.shape and out.device == m.codes.device, f"out must be a {m.rows} x {m.cols} tensor on the codes' device")
-        q.use(m.codes, m.scales, m.zeros, out)
-        _check(lib().lpmm_w4_dequantize(m._ref, out.data_ptr(), _dtype_of(out, "out"), _rows_of(out, "out"), q.ptr), "lpmm_w4_dequantize")
+    if not _here(stream, m.device):
+        with _elsewhere(stream, m.device, m.codes, m.scales, m.zeros, out):
+            return w4_dequantize(m, dtype, out=out)
+    if out is None:
+        _need(dtype in _DTYPE, "dtype must be float32, bfloat16 or float16")
+        out = m.codes.new_empty((m.rows, m.cols), dtype=dtype)
+    else:
+        _need(out.shape == m.shape and out.device == m.device, f"out must be a {m.rows} x {m.cols} tensor on the codes' device")
+    _check(lib().lpmm_w4_dequantize(m._ref, out.data_ptr(), _dtype_of(out, "out"), _rows_of(out, "out"), _raw_stream(m.device)),
+           "lpmm_w4_dequantize")
     return out
 
 
 def w4_matvec(m: W4Matrix, x: torch.Tensor, *, bias=None, out=None, out_dtype=None, stream=None) -> torch.Tensor:
     """lpmm_w4_matvec: x W^T + bias for activations x (cols, or tokens x cols with contiguous rows) of float32, bfloat16 or
     float16. The result has x's type, or float32 with out_dtype=torch.float32 (or `out`)."""
-    _need(x.dim() in (1, 2) and x.shape[-1] == m.cols and x.device == m.codes.device, f"x must have {m.cols} columns and lie on the codes' device")
-    x2 = x if x.dim() == 2 else x.unsqueeze(0)
-    tokens = x2.shape[0]
+    shape, device = x.shape, m.device
+    if len(shape) not in (1, 2) or shape[-1] != m.cols or x.device != device:
+        raise ValueError(f"x must have {m.cols} columns and lie on the codes' device")
+    if not _here(stream, device):
+        with _elsewhere(stream, device, m.codes, m.scales, m.zeros, x, bias, out):
+            return w4_matvec(m, x, bias=bias, out=out, out_dtype=out_dtype)
+    if len(shape) == 1:
+        tokens, x_stride = 1, m.cols
+        _need(m.cols <= 1 or x.stride(0) == 1, "x must be contiguous")
+        shape = (m.rows,)
+    else:
+        tokens, x_stride = shape[0], _rows_of(x, "x")
+        shape = (tokens, m.rows)
     if bias is not None:
-        _need(bias.shape == (m.rows,) and bias.dtype == torch.float32 and bias.is_contiguous() and bias.device == x.device,
+        _need(bias.shape == (m.rows,) and bias.dtype == torch.float32 and bias.is_contiguous() and bias.device == device,
               f"bias must be a contiguous float32 tensor of {m.rows} elements on x's device")
-    with _Enqueue(stream, x.device) as q:
-        shape = (m.rows,) if x.dim() == 1 else (tokens, m.rows)
-        if out is None:
-            out = torch.empty(shape, dtype=out_dtype or x.dtype, device=x.device)
+    y_stride = m.rows
+    if out is None:
+        out = x.new_empty(shape, dtype=out_dtype)
+    else:
+        _need(out.shape == shape and out.device == device and out_dtype in (None, out.dtype), f"out must be a {shape} tensor on x's device")
+        if len(shape) == 2:
+            y_stride = _rows_of(out, "out")
         else:
-            _need(out.shape == shape and out.device == x.device and out_dtype in (None, out.dtype), f"out must be a {shape} tensor on x's device")
-        out2 = out if x.dim() == 2 else out.unsqueeze(0)
-        _need(out.dtype in (x.dtype, torch.float32), "the result must have x's type or float32")
-        q.use(m.codes, m.scales, m.zeros, x, bias, out)
-        _check(lib().lpmm_w4_matvec(m._ref, x2.data_ptr(), _dtype_of(x, "x"), _rows_of(x2, "x"), tokens,
-                                    None if bias is None else bias.data_ptr(), out2.data_ptr(), _DTYPE[out.dtype],
-                                    _rows_of(out2, "out"), q.ptr), "lpmm_w4_matvec")
+            _need(m.rows <= 1 or out.stride(0) == 1, "out must be contiguous")
+    xd, yd = _dtype_of(x, "x"), _DTYPE.get(out.dtype)
+    _need(yd == xd or yd == F32, "the result must have x's type or float32")
+    _check(lib().lpmm_w4_matvec(m._ref, x.data_ptr(), xd, x_stride, tokens, None if bias is None else bias.data_ptr(),
+                                out.data_ptr(), yd, y_stride, _raw_stream(device)), "lpmm_w4_matvec")
     return out
 
 
 def _distill(logits, top_ids, top_logits, temperature, teacher_lse, weights, grad, stream):
     _need(logits.is_cuda and logits.dim() == 2 and logits.shape[1] > 0, "logits must be a tokens x vocabulary CUDA tensor")
+    device = logits.device
+    if not _here(stream, device):
+        with _elsewhere(stream, device, logits, top_ids, top_logits, teacher_lse, weights, grad if grad is not True else None):
+            return _distill(logits, top_ids, top_logits, temperature, teacher_lse, weights, grad, None)
     tokens, vocab = logits.shape
-    dtype, stride = _dtype_of(logits, "logits"), _rows_of(logits, "logits")
-    _need(top_ids.dim() == 2 and top_ids.shape[0] == tokens and top_ids.shape == top_logits.shape, "top_ids and top_logits must be tokens x top")
-    _need(top_ids.dtype in (torch.int32, torch.int64), "top_ids must be int32 or int64")
-    for name, t in (("top_ids", top_ids), ("top_logits", top_logits), ("teacher_lse", teacher_lse), ("weights", weights)):
-        if t is not None:
-            _need(t.is_contiguous() and t.device == logits.device, f"{name} must be contiguous and on the logits' device")
-    for name, t in (("teacher_lse", teacher_lse), ("weights", weights)):
-        if t is not None:
-            _need(t.shape == (tokens,) and t.dtype == torch.float32, f"{name} must be a float32 tensor of {tokens} elements")
-    with _Enqueue(stream, logits.device) as q:
-        loss = torch.empty(tokens, dtype=torch.float32, device=logits.device)
-        args = (logits.data_ptr(), dtype, stride, tokens, vocab, top_ids.data_ptr(), top_ids.element_size(), top_logits.data_ptr(),
-                _dtype_of(top_logits, "top_logits"), top_ids.shape[1], None if teacher_lse is None else teacher_lse.data_ptr(),
-                None if weights is None else weights.data_ptr(), temperature, loss.data_ptr())
-        q.use(logits, top_ids, top_logits, teacher_lse, weights)
-        if grad is None:
-            _check(lib().lpmm_distill_loss(*args, q.ptr), "lpmm_distill_loss")
-            return loss, None
-        if grad is True:
-            grad = torch.empty(tokens, vocab, dtype=logits.dtype, device=logits.device)
-        else:
-            _need(grad.shape == logits.shape and grad.dtype == logits.dtype and grad.device == logits.device, "out must match the logits")
-            q.use(grad)
-        _check(lib().lpmm_distill_grad(*args, grad.data_ptr(), _rows_of(grad, "out"), q.ptr), "lpmm_distill_grad")
+    shape = top_ids.shape
+    if len(shape) != 2 or shape[0] != tokens or shape != top_logits.shape:
+        raise ValueError("top_ids and top_logits must be tokens x top")
+    ids_bytes = 8 if top_ids.dtype == torch.int64 else 4 if top_ids.dtype == torch.int32 else 0
+    _need(ids_bytes, "top_ids must be int32 or int64")
+    lse = wts = None
+    if not (top_ids.is_contiguous() and top_logits.is_contiguous() and top_ids.device == device and top_logits.device == device):
+        raise ValueError("top_ids and top_logits must be contiguous and on the logits' device")
+    if teacher_lse is not None:
+        lse = _per_row(teacher_lse, "teacher_lse", tokens, device)
+    if weights is not None:
+        wts = _per_row(weights, "weights", tokens, device)
+    loss = logits.new_empty(tokens, dtype=torch.float32)
+    args = (logits.data_ptr(), _dtype_of(logits, "logits"), _rows_of(logits, "logits"), tokens, vocab, top_ids.data_ptr(), ids_bytes,
+            top_logits.data_ptr(), _dtype_of(top_logits, "top_logits"), shape[1], lse, wts, temperature, loss.data_ptr())
+    if grad is None:
+        _check(lib().lpmm_distill_loss(*args, _raw_stream(device)), "lpmm_distill_loss")
+        return loss, None
+    if grad is True:
+        grad, stride = logits.new_empty((tokens, vocab)), vocab
+    else:
+        _need(grad.shape == logits.shape and grad.dtype == logits.dtype and grad.device == device, "out must match the logits")
+        stride = _rows_of(grad, "out")
+    _check(lib().lpmm_distill_grad(*args, grad.data_ptr(), stride, _raw_stream(device)), "lpmm_distill_grad")
     return loss, grad
+
+
+def _per_row(t, name, tokens, device):
+    if t.shape != (tokens,) or t.dtype != torch.float32 or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous float32 tensor of {tokens} elements on the logits' device")
+    return t.data_ptr()
 
 
 def distill_loss(logits, top_ids, top_logits, *, temperature=1.0, teacher_lse=None, weights=None, stream=None) -> torch.Tensor:
