@@ -145,8 +145,8 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
 //
 // One CTA per SM holds the activations in shared memory and goes through tiles of 16 rows; its warps share out the stages (16 rows
 // by 512 columns, 4 KB of codes) of all its tiles evenly, in order, each streaming its own through two or three buffers of its
-// own in shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. A lane reads one 32-bit word =
-// 8 codes of one row per 32 columns; the pairs that its halves hold, (0, 4), (1, 5), (2, 6), (3, 7), are brought to the tensor
+// own in shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. The four lanes of a
+// row take consecutive quarters of a group's codes, 8 codes = a 32-bit word per product; the pairs that its halves hold, (0, 4), (1, 5), (2, 6), (3, 7), are brought to the tensor
 // cores' operand by a mask and one exact multiply-add. The order of the columns inside a product is free as long as both operands
 // have the same: the activations' pairs are put into that order.
 //
@@ -163,10 +163,10 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a));
     return r;
 }
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-    uint32_t r;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r) : "r"(a));
-    return r;
+template <int N> __device__ __forceinline__ void lds_words(uint32_t a, uint32_t (&w)[N]) {
+    if constexpr (N == 1) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(a));
+    else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a));
+    else asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a));
 }
 __device__ __forceinline__ float ld_rank(uint32_t a, uint32_t rank) {    // the same place in CTA `rank`'s shared memory
     float v;
@@ -235,6 +235,10 @@ template <> struct Codes<__nv_bfloat16> {
 
 template <typename T> struct Operand { using M = T; static constexpr int parts = 1; };
 template <> struct Operand<float> { using M = __nv_bfloat16; static constexpr int parts = 3; };
+
+// Rows lie 256 bytes apart in a stage; its 16-byte pieces are permuted by the row, so that whatever the lanes of a warp read at a
+// time (4, 8 or 16 bytes from each of 8, 4 or 2 rows) lies on different banks: the row's three low bits, reversed.
+__device__ __forceinline__ int row_swizzle(int r) { return (r & 1) << 2 | (r & 2) | (r & 4) >> 2; }
 
 struct W4Product {
     W4Quant w;           // w.w: the activations, w.w_stride: their rows' distance
@@ -312,8 +316,7 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
     float* const sums = reinterpret_cast<float*>(smem + warps * (DEPTH * kStage) + p.block_tokens * PARTS * p.x_pitch + kZeroLine);
     const int slot_floats = p.block_tokens * PARTS * kColPitch;
 
-    // Codes: lane l copies 16 bytes of rows l / 16, l / 16 + 2, ...; a row's 16-byte pieces are permuted by the row number, so that the
-    // eight rows a warp reads at a time lie on different banks. What lies behind the last row or column is read from the last
+    // Codes: lane l copies 16 bytes of rows l / 16, l / 16 + 2, ... What lies behind the last row or column is read from the last
     // one instead: its sums are not used, its activations are zeros.
     const int last_byte = ((cols + 1) / 2 - 1) & ~15, my_byte = (lane & 15) * 16;
     const uint8_t* f_base;
@@ -335,7 +338,7 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
             const uint8_t* const src = f_base + min((st0 + f_st) * kStageBytes + my_byte, last_byte);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(o + i * 2 * kStageBytes + (((lane & 15) ^ ((i * 2 + (lane >> 4)) & 7)) << 4)), "l"(src + f_off[i]) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(o + i * 2 * kStageBytes + (((lane & 15) ^ row_swizzle(i * 2 + (lane >> 4))) << 4)), "l"(src + f_off[i]) : "memory");
             if (++f_st == stages) { f_st = 0; ++f_tile; fetch_rows(); }
             ++fu;
         }
@@ -385,7 +388,8 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
             const int e = e0 + shift < eights ? e0 + shift : e0 + shift - eights, k = st0 * kStageCols + e * 8;
             for (int mb = threadIdx.x >> p.log_run; mb < mcount; mb += BATCH * m_step) {
                 const T* src = static_cast<const T*>(a.w) + (m0 + mb) * a.w_stride;
-                const uint32_t dst = xs + mb * PARTS * p.x_pitch + e * 16;
+                // where the product that has eight t * GB + i of a group for lane t reads it: place 4 i + t of the group
+                const uint32_t dst = xs + mb * PARTS * p.x_pitch + ((e & ~(4 * GB - 1)) | (e & (GB - 1)) << 2 | (e / GB & 3)) * 16;
                 if constexpr (PARTS == 1) {
                     uint4 v[BATCH];
 #pragma unroll
@@ -436,13 +440,14 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
         __syncwarp();
         float nsa[NS] = {}, nsb[NS] = {}, nza[NS] = {}, nzb[NS] = {};
         if (u + 1 < u1) load_scales(nsa, nsb, nza, nzb);
-        const uint32_t codes = ring + slot + g * kStageBytes + (g << 4) + t * 4;
+        const uint32_t codes = (ring + slot + g * kStageBytes + t * (4 * GB)) ^ (row_swizzle(g) << 4);
         slot = slot == (DEPTH - 1) * kStage ? 0 : slot + kStage;
         uint32_t xa[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) xa[n] = xcol[n] + st * xstep[n];
         float part[NT][4];
         float s0 = 0.0f, s1 = 0.0f;
+        uint32_t wa[GB], wb[GB];
 #pragma unroll
         for (int b = 0; b < kStageCols / 32; ++b) {
             if (b % GB == 0) {        // a new group
@@ -454,9 +459,13 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
                     Codes<M>::zero_operand(__shfl_sync(0xffffffffu, zb[i], from), z1, z1x);
                 }
             }
+            if (b % GB == 0) {        // this lane's quarter of the group, of rows g and g + 8 (b * 16 reaches above the permuted bits: no carry)
+                lds_words<GB>(codes ^ (b * 16), wa);
+                lds_words<GB>((codes ^ (b * 16)) + 8 * kStageBytes, wb);
+            }
             uint32_t qa[4], qb[4];
-            Codes<M>::expand(lds32(codes ^ (b << 4)), z0, z0x, qa);
-            Codes<M>::expand(lds32((codes ^ (b << 4)) + 8 * kStageBytes), z1, z1x, qb);
+            Codes<M>::expand(wa[b % GB], z0, z0x, qa);
+            Codes<M>::expand(wb[b % GB], z1, z1x, qb);
             const uint32_t a0[4] = {qa[0], qb[0], qa[1], qb[1]}, a1[4] = {qa[2], qb[2], qa[3], qb[3]};
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
