@@ -144,8 +144,7 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
 // (8 significant bits each), as three columns instead of one.
 //
 // One CTA per SM holds the activations in shared memory and goes through tiles of 16 rows; its warps share out the stages (16 rows
-// by 512 columns, 4 KB of codes) of all its tiles evenly, in order, each streaming its own through two or three buffers of its
-// own in shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. The four lanes of a
+// by 512 columns, 4 KB of codes) of all its tiles evenly, in order, each streaming its own through two buffers of its own in shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. The four lanes of a
 // row take consecutive quarters of a group's codes, 8 codes = a 32-bit word per product; the pairs that its halves hold, (0, 4), (1, 5), (2, 6), (3, 7), are brought to the tensor
 // cores' operand by a mask and one exact multiply-add. The order of the columns inside a product is free as long as both operands
 // have the same: the activations' pairs are put into that order.
@@ -155,6 +154,7 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
 
 constexpr int kStageCols = 512, kStageBytes = kStageCols / 2;   // columns of one stage; its bytes per row
 constexpr int kStage = 16 * kStageBytes;                        // 4 KB
+constexpr int kDepth = 2;                                       // stages that a warp holds, the one it works on among them
 constexpr int kXPad = 64;                                       // bytes between columns: neighbouring columns on other banks
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -257,17 +257,19 @@ struct W4Product {
 constexpr int kZeroLine = 1024;     // bytes of zeros that are read in place of columns that are not there
 constexpr int kColPitch = 20;      // floats between the columns of 16 sums: the four lanes of a row on different banks
 constexpr int kMaxWarps = 16;
+constexpr int kMaxColumns = 16;    // 32 with half the warps: 4096 x 11008, 32 tokens 72 us, against 48 us with two passes over the codes
 
 // The warp that has unit u of `units` spread over `warps` (each has [units w / warps, units (w + 1) / warps)).
 __device__ __forceinline__ int warp_of(int u, int units, int warps) { return ((u + 1) * warps - 1) / units; }
 
-// Eight activations of fp32 as bfloat16 parts: the upper half of the bits is one, and what it leaves is exact. v keeps that.
-__device__ __forceinline__ uint4 take_part(float (&v)[8]) {
+// Eight fp32 activations as bfloat16 parts: the upper half of the bits is one, and what it leaves is exact. v keeps that.
+__device__ __forceinline__ uint4 take_part(uint32_t (&v)[8]) {
     uint32_t hi[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        hi[j] = __float_as_uint(v[j]) & 0xffff0000u;
-        v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - __uint_as_float(hi[j]);
+        hi[j] = v[j] & 0xffff0000u;
+        const float x = __uint_as_float(v[j]);
+        v[j] = fabsf(x) == INFINITY ? 0u : __float_as_uint(x - __uint_as_float(hi[j]));
     }
     return make_uint4((hi[0] >> 16) | hi[4], (hi[1] >> 16) | hi[5], (hi[2] >> 16) | hi[6], (hi[3] >> 16) | hi[7]);
 }
@@ -275,23 +277,31 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
-// Eight consecutive 16-bit elements of a row from column c on, as they are; zeros behind the row's end.
-template <typename T>
-__device__ __forceinline__ uint4 load8_bits(const T* row, int c, int cols, bool vec) {
-    if (vec && c + 8 <= cols) return __ldg(reinterpret_cast<const uint4*>(row + c));
-    const unsigned short* const u = reinterpret_cast<const unsigned short*>(row);
-    uint32_t v[8];
+// Eight consecutive elements of a row from column c on, as they are; zeros behind the row's end.
+template <typename T, int N>
+__device__ __forceinline__ void load8_bits(const T* row, int c, int cols, bool vec, uint4 (&v)[N]) {
+    if (vec && c + 8 <= cols) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? __ldg(u + c + i) : 0u;
-    return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+        for (int i = 0; i < N; ++i) v[i] = __ldg(reinterpret_cast<const uint4*>(row + c) + i);
+    } else if constexpr (sizeof(T) == 4) {
+        const uint32_t* const u = reinterpret_cast<const uint32_t*>(row);
+        uint32_t e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? __ldg(u + c + i) : 0u;
+        v[0] = make_uint4(e[0], e[1], e[2], e[3]);
+        v[1] = make_uint4(e[4], e[5], e[6], e[7]);
+    } else {
+        const unsigned short* const u = reinterpret_cast<const unsigned short*>(row);
+        uint32_t e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? __ldg(u + c + i) : 0u;
+        v[0] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    }
 }
 
 // GB: 32-column blocks per scale (1, 2 or 4; wider groups repeat their scale). NT: tiles of 8 columns of activations.
-// DEPTH: stages a warp holds, the one it works on among them. Wide products (NT = 4) run with 8 warps and twice the registers: 12 of
-// a group's sums and as many of a row's stay in registers beside the operands of several blocks.
-constexpr int most_warps(int nt) { return nt == 4 ? 8 : kMaxWarps; }
-template <typename T, int NT, int GB, int DEPTH>
-__global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(const W4Product p) {
+template <typename T, int NT, int GB>
+__global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4Product p) {
     using M = typename Operand<T>::M;
     constexpr int PARTS = Operand<T>::parts;
     constexpr int NS = 4 / GB;         // scales per row, stage and lane: the four lanes of a row hold a stage's
@@ -310,10 +320,10 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
     const int mcount = (int)min((int64_t)p.block_tokens, p.tokens - m0), ncols = mcount * PARTS;
 
     // Shared memory: the warps' buffers (later the CTA's sums), the activations, zeros, the sums of (tile, warp) pairs.
-    const uint32_t ring = smem_u32(smem) + warp * (DEPTH * kStage);
-    const uint32_t xs = smem_u32(smem) + warps * (DEPTH * kStage);
+    const uint32_t ring = smem_u32(smem) + warp * (kDepth * kStage);
+    const uint32_t xs = smem_u32(smem) + warps * (kDepth * kStage);
     const uint32_t zero_line = xs + p.block_tokens * PARTS * p.x_pitch;
-    float* const sums = reinterpret_cast<float*>(smem + warps * (DEPTH * kStage) + p.block_tokens * PARTS * p.x_pitch + kZeroLine);
+    float* const sums = reinterpret_cast<float*>(smem + warps * (kDepth * kStage) + p.block_tokens * PARTS * p.x_pitch + kZeroLine);
     const int slot_floats = p.block_tokens * PARTS * kColPitch;
 
     // Codes: lane l copies 16 bytes of rows l / 16, l / 16 + 2, ... What lies behind the last row or column is read from the last
@@ -334,7 +344,7 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
     const auto fetch = [&] {
         if (fu < u1) {
             const uint32_t o = ring + f_slot + (lane >> 4) * kStageBytes;
-            f_slot = f_slot == (DEPTH - 1) * kStage ? 0 : f_slot + kStage;
+            f_slot = f_slot == (kDepth - 1) * kStage ? 0 : f_slot + kStage;
             const uint8_t* const src = f_base + min((st0 + f_st) * kStageBytes + my_byte, last_byte);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -344,8 +354,6 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-#pragma unroll
-    for (int i = 0; i < DEPTH - 1; ++i) fetch();
 
     // Scales (and zero points) of a stage, one stage ahead, in registers: lane t of a row holds groups t NS to t NS + NS - 1.
     int s_tile = tile0 + first_tile, s_st = first_stage;
@@ -379,44 +387,53 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
 
     // The activations of this CTA's columns, eight at a time: 2^log_run threads side by side take a token's, several tokens' loads
     // are under way at once, and the clusters start at different places, so that they do not all ask the same part of the L2
-    // cache at a time.
-    for (int i = threadIdx.x; i < kZeroLine / 16; i += blockDim.x) sts128(zero_line + i * 16, make_uint4(0, 0, 0, 0));
-    {
-        constexpr int BATCH = PARTS == 1 ? 8 : 4;
-        const int eights = stages * (kStageCols / 8), run = 1 << p.log_run, m_step = blockDim.x >> p.log_run, shift = (cluster * 13) % eights;
-        for (int e0 = threadIdx.x & (run - 1); e0 < eights; e0 += run) {
-            const int e = e0 + shift < eights ? e0 + shift : e0 + shift - eights, k = st0 * kStageCols + e * 8;
-            for (int mb = threadIdx.x >> p.log_run; mb < mcount; mb += BATCH * m_step) {
-                const T* src = static_cast<const T*>(a.w) + (m0 + mb) * a.w_stride;
-                // where the product that has eight t * GB + i of a group for lane t reads it: place 4 i + t of the group
-                const uint32_t dst = xs + mb * PARTS * p.x_pitch + ((e & ~(4 * GB - 1)) | (e & (GB - 1)) << 2 | (e / GB & 3)) * 16;
-                if constexpr (PARTS == 1) {
-                    uint4 v[BATCH];
+    // cache at a time. The first loads go out before the codes', behind which they would queue.
+    constexpr int BATCH = PARTS == 1 ? 8 : 4;
+    const int eights = stages * (kStageCols / 8), m_step = blockDim.x >> p.log_run, my_m = threadIdx.x >> p.log_run;
+    const int shift = cluster * 16 % eights;
+    int xe = my_m < mcount ? threadIdx.x & ((1 << p.log_run) - 1) : eights, xm = my_m;
+    uint4 xv[BATCH][PARTS == 1 ? 1 : 2];
+    const auto x_place = [&] { return xe + shift < eights ? xe + shift : xe + shift - eights; };
+    const auto load_x = [&] {
+        if (xe >= eights) return;
+        const int k = st0 * kStageCols + x_place() * 8;
 #pragma unroll
-                    for (int j = 0; j < BATCH; ++j)
-                        v[j] = mb + j * m_step < mcount ? load8_bits(src + j * m_step * a.w_stride, k, cols, a.vec) : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < BATCH; ++j)
+            if (xm + j * m_step < mcount) load8_bits(static_cast<const T*>(a.w) + (m0 + xm + j * m_step) * a.w_stride, k, cols, a.vec, xv[j]);
+    };
+    const auto store_x = [&] {
+        // where the product that has eight t * GB + i of a group for lane t reads it: place 4 i + t of the group
+        const int e = x_place();
+        const uint32_t dst = xs + xm * PARTS * p.x_pitch + ((e & ~(4 * GB - 1)) | (e & (GB - 1)) << 2 | (e / GB & 3)) * 16;
 #pragma unroll
-                    for (int j = 0; j < BATCH; ++j)
-                        if (mb + j * m_step < mcount)
-                            sts128(dst + j * m_step * p.x_pitch, make_uint4(__byte_perm(v[j].x, v[j].z, 0x5410), __byte_perm(v[j].x, v[j].z, 0x7632),
-                                                                            __byte_perm(v[j].y, v[j].w, 0x5410), __byte_perm(v[j].y, v[j].w, 0x7632)));
-                } else {
-                    float v[BATCH][8];
+        for (int j = 0; j < BATCH; ++j) {
+            if (xm + j * m_step >= mcount) break;
+            if constexpr (PARTS == 1) {
+                const uint4 v = xv[j][0];
+                sts128(dst + j * m_step * p.x_pitch, make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632),
+                                                                __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632)));
+            } else {
+                uint32_t v[8] = {xv[j][0].x, xv[j][0].y, xv[j][0].z, xv[j][0].w, xv[j][1].x, xv[j][1].y, xv[j][1].z, xv[j][1].w};
 #pragma unroll
-                    for (int j = 0; j < BATCH; ++j)
-                        if (mb + j * m_step < mcount) load8(src + j * m_step * a.w_stride, k, cols, a.vec, v[j]);
-#pragma unroll
-                    for (int j = 0; j < BATCH; ++j) {
-                        if (mb + j * m_step >= mcount) break;
-#pragma unroll
-                        for (int part = 0; part < PARTS; ++part) sts128(dst + (j * m_step * PARTS + part) * p.x_pitch, take_part(v[j]));
-                    }
-                }
+                for (int part = 0; part < PARTS; ++part) sts128(dst + (j * m_step * PARTS + part) * p.x_pitch, take_part(v));
             }
         }
-    }
+    };
+    load_x();
     float sa[NS], sb[NS], za[NS], zb[NS];
     if (u0 < u1) load_scales(sa, sb, za, zb);
+#pragma unroll
+    for (int i = 0; i < kDepth - 1; ++i) fetch();
+    for (int i = threadIdx.x; i < kZeroLine / 16; i += blockDim.x) sts128(zero_line + i * 16, make_uint4(0, 0, 0, 0));
+    while (xe < eights) {
+        store_x();
+        xm += BATCH * m_step;
+        if (xm >= mcount) {
+            xm = my_m;
+            xe += 1 << p.log_run;
+        }
+        load_x();
+    }
     __syncthreads();
 
     uint32_t xcol[NT], xstep[NT];
@@ -436,12 +453,12 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
     uint32_t slot = 0;
     for (int u = u0; u < u1; ++u) {
         fetch();
-        asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
         __syncwarp();
         float nsa[NS] = {}, nsb[NS] = {}, nza[NS] = {}, nzb[NS] = {};
         if (u + 1 < u1) load_scales(nsa, nsb, nza, nzb);
         const uint32_t codes = (ring + slot + g * kStageBytes + t * (4 * GB)) ^ (row_swizzle(g) << 4);
-        slot = slot == (DEPTH - 1) * kStage ? 0 : slot + kStage;
+        slot = slot == (kDepth - 1) * kStage ? 0 : slot + kStage;
         uint32_t xa[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) xa[n] = xcol[n] + st * xstep[n];
@@ -549,43 +566,41 @@ __global__ void __launch_bounds__(most_warps(NT) * 32, 1) w4_product_kernel(cons
     if (ranks > 1) asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
-// How a product is laid out: CTAs per cluster, clusters, warps per CTA, stages that a warp holds, shared memory.
+// How a product is laid out: CTAs per cluster, clusters, warps per CTA, shared memory.
 struct ProductPlan {
-    int ranks, clusters, warps, depth;
+    int ranks, clusters, warps;
     size_t bytes;
     int64_t cost;
 };
 
-// The layout with the fewest stages per CTA (as its busiest warp has them) among those that fit, and a little for each cluster's
-// last exchange. Clusters of 1, 2, 4 and 8 that run side by side at one CTA per SM: 148, 74, 33 and 15 on this part. A third
-// stage per warp, where it fits, keeps more of HBM's latency covered (32000 x 4096, one token: 22.5 us with two stages).
+// The layout with the fewest stages per CTA (as its busiest warp has them; eight warps take half as long again per stage as
+// sixteen do: 11008 x 4096, eight tokens, 16.4 against 14.3 us) among those that fit, and a little for each cluster's last exchange. Clusters of 1, 2, 4 and 8 that run side by side at one CTA per SM: 148, 74, 33 and 15 on this part.
 ProductPlan plan_product(int64_t rows, int64_t cols, int columns, int64_t blocks) {
     const int side_by_side[4] = {148, 74, 33, 15};
     const int64_t tiles = (rows + 15) / 16, stages = (cols + kStageCols - 1) / kStageCols, room = 227 * 1024 - 1024;
-    const int warps = columns > 16 ? 8 : kMaxWarps;
-    ProductPlan best = {0, 0, 0, 0, 0, INT64_MAX};
+    ProductPlan best = {0, 0, 0, 0, INT64_MAX};
     for (int i = 0; i < 4; ++i) {
         const int ranks = 1 << i;
         if (ranks > stages && i) break;
         const int64_t ns = (stages + ranks - 1) / ranks, slot = (int64_t)columns * kColPitch * 4;
-        for (int depth = 3; depth >= 2; --depth) {
-            const int64_t ring = (int64_t)warps * depth * kStage, fixed = ring + columns * (ns * kStageCols * 2 + kXPad) + kZeroLine;
+        for (int warps = kMaxWarps; warps >= 8; warps -= 8) {
+            const int64_t ring = (int64_t)warps * kDepth * kStage, fixed = ring + columns * (ns * kStageCols * 2 + kXPad) + kZeroLine;
             // tiles whose sums fit, by warp behind the rest and by CTA into the buffers
             const int64_t fit = std::min((room - fixed) / slot - warps, ring / (columns * 64));
             if (fixed > room || fit < 1) continue;
             const int64_t at_a_time = std::max<int64_t>(1, side_by_side[i] / blocks);
             const int64_t per = std::min((tiles + at_a_time - 1) / at_a_time, fit), clusters = (tiles + per - 1) / per;
             const int64_t waves = (clusters * blocks + side_by_side[i] - 1) / side_by_side[i];
-            const int64_t cost = waves * (2 * warps * ((per * ns + warps - 1) / warps) + 16 + 8 * i);
-            if (cost < best.cost) best = {ranks, (int)clusters, warps, depth, (size_t)(fixed + (per + warps) * slot), cost};
+            const int64_t cost = waves * ((warps == kMaxWarps ? 2 : 3) * warps * ((per * ns + warps - 1) / warps) + 16 + 8 * i);
+            if (cost < best.cost) best = {ranks, (int)clusters, warps, (size_t)(fixed + (per + warps) * slot), cost};
         }
     }
     return best;
 }
 
-template <typename T, int NT, int GB, int DEPTH>
+template <typename T, int NT, int GB>
 cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t blocks, cudaStream_t s) {
-    auto kernel = w4_product_kernel<T, NT, GB, DEPTH>;
+    auto kernel = w4_product_kernel<T, NT, GB>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.bytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -601,11 +616,6 @@ cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t 
     cfg.numAttrs = plan.ranks > 1 ? 1 : 0;
     e = cudaLaunchKernelEx(&cfg, kernel, p);
     return e != cudaSuccess ? e : cudaGetLastError();
-}
-
-template <typename T, int NT, int GB>
-cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t blocks, cudaStream_t s) {
-    return plan.depth == 3 ? launch_product<T, NT, GB, 3>(p, plan, blocks, s) : launch_product<T, NT, GB, 2>(p, plan, blocks, s);
 }
 
 W4Quant pack_args(const W4Matrix& m, const void* w, int64_t stride, int es) {
@@ -647,8 +657,8 @@ cudaError_t launch_w4_matvec(const W4Matrix& m, const void* x, int x_dtype, int6
         p.tokens = tokens; p.bias = bias; p.y = y; p.y_stride = y_stride;
         p.scale_dtype = m.scale_dtype;
         p.y_f32 = y_dtype == 0;
-        // Up to 32 columns of activations at a time (a token is PARTS of them), as few as fit beside the rings.
-        int64_t block = std::min<int64_t>(tokens, 32 / PARTS), blocks;
+        // Up to 16 columns of activations at a time (a token is PARTS of them), as few as fit beside the rings.
+        int64_t block = std::min<int64_t>(tokens, kMaxColumns / PARTS), blocks;
         ProductPlan plan;
         for (;; block = (block + 1) / 2) {
             blocks = std::min<int64_t>((tokens + block - 1) / block, 65535);
@@ -682,8 +692,7 @@ cudaError_t launch_w4_matvec(const W4Matrix& m, const void* x, int x_dtype, int6
         };
         const int64_t columns = block * PARTS;
         if (columns <= 8) return run(std::integral_constant<int, 1>{});
-        if (columns <= 16) return run(std::integral_constant<int, 2>{});
-        return run(std::integral_constant<int, 4>{});
+        return run(std::integral_constant<int, 2>{});
     });
 }
 
