@@ -14,30 +14,43 @@ namespace lpmm {
 namespace {
 
 constexpr int kW4Threads = 256;
+constexpr int kW4Warps = kW4Threads / 32;
+constexpr int kSpan = 256;        // columns that a warp takes at a time, eight consecutive ones per lane = one 32-bit word of codes
 
-int w4_grid(int64_t blocks) { return (int)(blocks < 1 ? 1 : blocks > 148 * 16 ? 148 * 16 : blocks); }
+struct W4Quant {
+    const void* w;
+    int64_t w_stride;
+    uint8_t* codes;
+    void* scales;
+    uint8_t* zeros;
+    int64_t rows, cols, codes_stride, groups;
+    int32_t group, vec;
+    // Spans are numbered row by row, and a warp takes every so manieth: as rows and spans to go on by, so that nothing is divided.
+    int32_t spans, step_rows, step_spans;
+    int32_t log_group;      // -1: not a power of two up to 128
+    float one;              // 1, known at run time only (see pack_codes)
+};
 
-// ------------------------------------------------------------------------------------------------ quantizer
+// The spans of a warp, one after the other.
+struct SpanWalk {
+    int64_t row;
+    int span;
+    __device__ __forceinline__ SpanWalk(const W4Quant& a) {
+        const int64_t first = (int64_t)blockIdx.x * kW4Warps + (threadIdx.x >> 5);
+        row = first / a.spans;
+        span = (int)(first - row * a.spans);
+    }
+    __device__ __forceinline__ void next(const W4Quant& a) {
+        row += a.step_rows;
+        span += a.step_spans;
+        if (span >= a.spans) { span -= a.spans; ++row; }
+    }
+};
 
-// Scale of a group from its extremes (lo <= 0 <= hi), rounded to the type it is stored in; binary16 saturates instead of
-// overflowing, so that every value stays finite.
-template <typename S>
-__device__ __forceinline__ float group_scale(float lo, float hi, bool zeros) {
-    float s = zeros ? __fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f) : __fmul_rn(fmaxf(hi, -lo), 1.0f / 7.0f);
-    if constexpr (std::is_same<S, __half>::value) s = fminf(s, 65504.0f);
-    return to_f32(from_f32<S>(s));
-}
-__device__ __forceinline__ float group_zero(float lo, float rcp, bool zeros) {
-    return zeros ? fminf(fmaxf(rintf(__fmul_rn(-lo, rcp)), 0.0f), 15.0f) : 8.0f;
-}
-__device__ __forceinline__ uint32_t w4_code(float w, float rcp, float zero) {
-    return (uint32_t)fminf(fmaxf(__fadd_rn(rintf(__fmul_rn(w, rcp)), zero), 0.0f), 15.0f);
-}
-
-// Eight consecutive elements of a row from column c on; zeros behind the row's end.
+// Eight consecutive elements of a row from column c on, as binary32; zeros behind `end`.
 template <typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, bool vec, float (&v)[8]) {
-    if (vec && c + 8 <= cols) {
+__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t end, bool vec, float (&v)[8]) {
+    if (vec && c + 8 <= end) {
         if constexpr (sizeof(T) == 4) {
             const float4 a = __ldg(reinterpret_cast<const float4*>(row + c)), b = __ldg(reinterpret_cast<const float4*>(row + c) + 1);
             v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
@@ -52,86 +65,235 @@ __device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, boo
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (c + i < cols) ? to_f32(row[c + i]) : 0.0f;
+        for (int i = 0; i < 8; ++i) v[i] = (c + i < end) ? to_f32(row[c + i]) : 0.0f;
+    }
+}
+// The same for all lanes of a warp, c0 + 8 lane each, where rows are not aligned: neighbouring lanes load neighbouring elements and
+// hand them on through 256 floats of shared memory.
+template <typename T>
+__device__ __forceinline__ void load8_apart(const T* row, int64_t c0, int64_t end, float* tmp, float (&v)[8]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t c = c0 + i * 32 + lane;
+        tmp[i * 32 + lane] = c < end ? to_f32(row[c]) : 0.0f;
+    }
+    __syncwarp();
+    const float4 a = reinterpret_cast<const float4*>(tmp)[2 * lane], b = reinterpret_cast<const float4*>(tmp)[2 * lane + 1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    __syncwarp();
+}
+
+// ------------------------------------------------------------------------------------------------ quantizer
+//
+// Bound by HBM (bf16: 2.5 bytes per weight) as long as a weight takes fewer than 13 instructions: extremes of 16-bit types are
+// found two at a time in their own type; rint is an addition of 1.5 * 2^23, whose low bits then are the rounded value; eight
+// values are clamped to 0 .. 15 and packed by four instructions.
+
+// Scale of a group from its extremes (lo <= 0 <= hi), rounded to the type it is stored in; binary16 saturates instead of
+// overflowing, so that every value stays finite.
+template <typename S>
+__device__ __forceinline__ float group_scale(float lo, float hi, bool zeros) {
+    float s = zeros ? __fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f) : __fmul_rn(fmaxf(hi, -lo), 1.0f / 7.0f);
+    if constexpr (std::is_same<S, __half>::value) s = fminf(s, 65504.0f);
+    return to_f32(from_f32<S>(s));
+}
+__device__ __forceinline__ float group_zero(float lo, float rcp, bool zeros) {
+    return zeros ? fminf(fmaxf(rintf(__fmul_rn(-lo, rcp)), 0.0f), 15.0f) : 8.0f;
+}
+// The word of codes of eight weights. Values beyond +-2^21 (a saturated scale) are clamped before the addition that rounds; that
+// one is written as n * one + magic, since the assembler may join a packed product and a packed sum into one rounding.
+__device__ __forceinline__ uint32_t pack_codes(const float (&v)[8], float rcp, float zero, bool clamp, float one) {
+    constexpr float kMagic = 12582912.0f;
+    const int base = 0x4b400000 - (int)zero;
+    int q[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float2 n = mul2_rn(make_float2(v[2 * i], v[2 * i + 1]), splat(rcp));
+        if (clamp) n = make_float2(fminf(fmaxf(n.x, -64.0f), 64.0f), fminf(fmaxf(n.y, -64.0f), 64.0f));
+        n = fma2_rn(n, splat(one), splat(kMagic));
+        q[2 * i] = __float_as_int(n.x) - base;
+        q[2 * i + 1] = __float_as_int(n.y) - base;
+    }
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 6; i >= 0; i -= 2) asm("cvt.pack.sat.u4.s32.b32 %0, %1, %2, %0;" : "+r"(w) : "r"(q[i + 1]), "r"(q[i]));
+    return w;
+}
+// Extremes of eight weights, lo <= 0 <= hi.
+template <typename T>
+__device__ __forceinline__ void extremes(const float (&v)[8], float& lo, float& hi) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { lo = fminf(lo, v[i]); hi = fmaxf(hi, v[i]); }
+}
+template <typename T> struct Pair2;
+template <> struct Pair2<__nv_bfloat16> { using P = __nv_bfloat162; };
+template <> struct Pair2<__half> { using P = __half2; };
+template <typename T, bool MAX> __device__ __forceinline__ uint32_t pick2(uint32_t a, uint32_t b) {
+    using P = typename Pair2<T>::P;
+    const P x = *reinterpret_cast<const P*>(&a), y = *reinterpret_cast<const P*>(&b), r = MAX ? __hmax2(x, y) : __hmin2(x, y);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// Groups of 32, 64 and 128 columns: LANES = 4, 8 and 16 neighbouring lanes.
+template <typename T, typename S, int LANES>
+__global__ void __launch_bounds__(kW4Threads) w4_quantize_kernel(const W4Quant a) {
+    __shared__ __align__(16) float tmp[kW4Warps][kSpan];
+    const int lane = threadIdx.x & 31;
+    const bool zeros = a.zeros != nullptr;
+    SpanWalk at(a);
+#pragma unroll 2
+    for (; at.row < a.rows; at.next(a)) {
+        const T* const row = static_cast<const T*>(a.w) + at.row * a.w_stride;
+        const int64_t c0 = (int64_t)at.span * kSpan, c = c0 + lane * 8;
+        float v[8], lo = 0.0f, hi = 0.0f;
+        if (sizeof(T) == 2 && a.vec && c0 + kSpan <= a.cols) {
+            const uint4 q = __ldg(reinterpret_cast<const uint4*>(row + c));
+            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+            if constexpr (sizeof(T) == 2) {
+                if (zeros) {      // -lo and hi side by side
+                    const uint32_t mx = pick2<T, true>(pick2<T, true>(q.x, q.y), pick2<T, true>(q.z, q.w)), mn = pick2<T, false>(pick2<T, false>(q.x, q.y), pick2<T, false>(q.z, q.w));
+                    uint32_t m = __byte_perm(mx, mn, 0x5410), o = __byte_perm(mx, mn, 0x7632);
+                    m = pick2<T, true>(m ^ 0x80000000u, o ^ 0x80000000u);
+#pragma unroll
+                    for (int d = LANES / 2; d; d >>= 1) m = pick2<T, true>(m, __shfl_xor_sync(0xffffffffu, m, d));
+                    const float2 p = unpack_pair<T>(m);
+                    hi = fmaxf(p.x, 0.0f); lo = fminf(-p.y, 0.0f);
+                } else {          // the largest |w|
+                    uint32_t m = pick2<T, true>(pick2<T, true>(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu), pick2<T, true>(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu));
+#pragma unroll
+                    for (int d = LANES / 2; d; d >>= 1) m = pick2<T, true>(m, __shfl_xor_sync(0xffffffffu, m, d));
+                    const float2 p = unpack_pair<T>(m);
+                    hi = fmaxf(p.x, p.y);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 p = unpack_pair<T>(u[i]);
+                    v[2 * i] = p.x; v[2 * i + 1] = p.y;
+                }
+            }
+        } else {
+            if (a.vec) load8(row, c, a.cols, true, v);
+            else load8_apart(row, c0, a.cols, tmp[threadIdx.x >> 5], v);
+            extremes<T>(v, lo, hi);
+#pragma unroll
+            for (int d = LANES / 2; d; d >>= 1) {
+                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+            }
+        }
+        const float s = group_scale<S>(lo, hi, zeros);
+        const float rcp = scale_rcp(s), zero = group_zero(lo, rcp, zeros);
+        if (c >= a.cols) continue;
+        if ((lane & (LANES - 1)) == 0) {
+            const int64_t g = at.row * a.groups + at.span * (32 / LANES) + lane / LANES;
+            static_cast<S*>(a.scales)[g] = from_f32<S>(s);
+            if (zeros) a.zeros[g] = (uint8_t)zero;
+        }
+        uint32_t word = pack_codes(v, rcp, zero, std::is_same<S, __half>::value && s == 65504.0f, a.one);
+        if (c + 8 > a.cols) word &= 0xffffffffu >> (4 * (c + 8 - a.cols));
+        *reinterpret_cast<uint32_t*>(a.codes + at.row * a.codes_stride + (c >> 1)) = word;
     }
 }
 
-struct W4Quant {
-    const void* w;
-    int64_t w_stride;
-    uint8_t* codes;
-    void* scales;
-    uint8_t* zeros;
-    int64_t rows, cols, codes_stride, groups;
-    int32_t group, vec;
-};
-
-// One warp per `span` columns of a row, a lane owns eight consecutive columns (one 32-bit word of codes). Groups of 32, 64 and
-// 128 columns are 4, 8 and 16 neighbouring lanes; wider groups (multiples of 128) are walked twice by one warp.
+// Wider groups (multiples of 128 columns): a warp walks one twice.
 template <typename T, typename S>
-__global__ void __launch_bounds__(kW4Threads) w4_quantize_kernel(const W4Quant a) {
+__global__ void __launch_bounds__(kW4Threads) w4_quantize_wide_kernel(const W4Quant a) {
+    __shared__ __align__(16) float tmp[kW4Warps][kSpan];
     const int lane = threadIdx.x & 31;
-    const int64_t span = a.group > 128 ? a.group : 256;
-    const int64_t chunks = (a.cols + span - 1) / span;
-    const int lanes = a.group > 128 ? 32 : a.group / 8;
-    const int64_t items = a.rows * chunks;
-    for (int64_t it = (int64_t)blockIdx.x * (kW4Threads / 32) + (threadIdx.x >> 5); it < items; it += (int64_t)gridDim.x * (kW4Threads / 32)) {
-        const int64_t r = it / chunks, c0 = (it - r * chunks) * span;
-        const T* row = static_cast<const T*>(a.w) + r * a.w_stride;
-        const int64_t end = min(c0 + span, a.cols);
+    const bool zeros = a.zeros != nullptr;
+    float* const mine = tmp[threadIdx.x >> 5];
+    for (SpanWalk at(a); at.row < a.rows; at.next(a)) {
+        const T* const row = static_cast<const T*>(a.w) + at.row * a.w_stride;
+        const int64_t first = (int64_t)at.span * a.group, end = min(first + a.group, a.cols);
         float v[8], lo = 0.0f, hi = 0.0f;
-        for (int64_t c = c0 + lane * 8; c < end; c += 256) {
-            load8(row, c, end, a.vec, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) { lo = fminf(lo, v[i]); hi = fmaxf(hi, v[i]); }
+        for (int64_t c0 = first; c0 < end; c0 += kSpan) {
+            if (a.vec) load8(row, c0 + lane * 8, end, true, v);
+            else load8_apart(row, c0, end, mine, v);
+            extremes<T>(v, lo, hi);
         }
-        for (int d = lanes >> 1; d; d >>= 1) {
+        for (int d = 16; d; d >>= 1) {
             lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
             hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
         }
-        const float s = group_scale<S>(lo, hi, a.zeros != nullptr);
-        const float rcp = scale_rcp(s), zero = group_zero(lo, rcp, a.zeros != nullptr);
-        const int64_t c1 = c0 + lane * 8;
-        if (c1 < end && (lane & (lanes - 1)) == 0) {
-            const int64_t g = r * a.groups + c1 / a.group;
+        const float s = group_scale<S>(lo, hi, zeros);
+        const float rcp = scale_rcp(s), zero = group_zero(lo, rcp, zeros);
+        if (lane == 0) {
+            const int64_t g = at.row * a.groups + at.span;
             static_cast<S*>(a.scales)[g] = from_f32<S>(s);
-            if (a.zeros) a.zeros[g] = (uint8_t)zero;
+            if (zeros) a.zeros[g] = (uint8_t)zero;
         }
-        for (int64_t c = c1; c < end; c += 256) {
-            if (span > 256) load8(row, c, end, a.vec, v);
-            uint32_t word = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) word |= (c + i < end ? w4_code(v[i], rcp, zero) : 0u) << (4 * i);
-            *reinterpret_cast<uint32_t*>(a.codes + r * a.codes_stride + (c >> 1)) = word;
+        for (int64_t c0 = first; c0 < end; c0 += kSpan) {
+            const int64_t c = c0 + lane * 8;
+            if (a.vec) load8(row, c, end, true, v);
+            else load8_apart(row, c0, end, mine, v);
+            if (c >= end) continue;
+            uint32_t word = pack_codes(v, rcp, zero, std::is_same<S, __half>::value && s == 65504.0f, a.one);
+            if (c + 8 > a.cols) word &= 0xffffffffu >> (4 * (c + 8 - a.cols));
+            *reinterpret_cast<uint32_t*>(a.codes + at.row * a.codes_stride + (c >> 1)) = word;
         }
     }
 }
 
 // ---------------------------------------------------------------------------------------------- dequantizer
+//
+// A code at bits 4k of the mantissa of 2^23 is 2^23 + q 16^k; less 2^23 + z 16^k and times 16^-k it is q - z, all exact.
 
 template <typename T, typename S>
 __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant a, T* __restrict__ out, int64_t out_stride) {
-    const int64_t words = (a.cols + 7) / 8;
-    const int64_t items = a.rows * words;
-    for (int64_t it = (int64_t)blockIdx.x * kW4Threads + threadIdx.x; it < items; it += (int64_t)gridDim.x * kW4Threads) {
-        const int64_t r = it / words, c = (it - r * words) * 8;
-        const uint32_t q = __ldg(reinterpret_cast<const uint32_t*>(a.codes + r * a.codes_stride + (c >> 1)));
-        const int64_t g = r * a.groups + c / a.group;
-        const float s = to_f32(static_cast<const S*>(a.scales)[g]), z = a.zeros ? (float)a.zeros[g] : 8.0f;
-        T* o = out + r * out_stride + c;
-        float v[8];
+    __shared__ __align__(16) float tmp[kW4Warps][kSpan];
+    const int lane = threadIdx.x & 31;
+    SpanWalk at(a);
+#pragma unroll 2
+    for (; at.row < a.rows; at.next(a)) {
+        const int64_t c0 = (int64_t)at.span * kSpan;
+        const int c = at.span * kSpan + lane * 8, cols = (int)a.cols;
+        const bool in = c < cols;
+        float2 v[4];
+        if (in) {
+            const uint32_t q = __ldg(reinterpret_cast<const uint32_t*>(a.codes + at.row * a.codes_stride + (c >> 1)));
+            const int64_t g = at.row * a.groups + (a.log_group >= 0 ? c >> a.log_group : c / a.group);
+            const float s = to_f32(static_cast<const S*>(a.scales)[g]), z = a.zeros ? (float)a.zeros[g] : 8.0f;
+            const float2 z01 = make_float2(-8388608.0f - z, -8388608.0f - 16.0f * z), z23 = make_float2(-8388608.0f - 256.0f * z, -8388608.0f - 4096.0f * z);
+            const float2 f01 = make_float2(1.0f, 0.0625f), f23 = make_float2(1.0f / 256, 1.0f / 4096), s2 = splat(s);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(__fsub_rn((float)((q >> (4 * i)) & 15u), z), s);
-        if (a.vec && c + 8 <= a.cols) {
-            if constexpr (sizeof(T) == 4) {
-                reinterpret_cast<float4*>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
-                reinterpret_cast<float4*>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
-            } else {
-                *reinterpret_cast<uint4*>(o) = make_uint4(pack_pair<T>(v[0], v[1]), pack_pair<T>(v[2], v[3]), pack_pair<T>(v[4], v[5]), pack_pair<T>(v[6], v[7]));
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t w = q >> (16 * h);
+                uint32_t n[4];
+                asm("lop3.b32 %0, %1, 0xf, 0x4b000000, 0xEA;" : "=r"(n[0]) : "r"(w));
+                asm("lop3.b32 %0, %1, 0xf0, 0x4b000000, 0xEA;" : "=r"(n[1]) : "r"(w));
+                asm("lop3.b32 %0, %1, 0xf00, 0x4b000000, 0xEA;" : "=r"(n[2]) : "r"(w));
+                asm("lop3.b32 %0, %1, 0xf000, 0x4b000000, 0xEA;" : "=r"(n[3]) : "r"(w));
+                v[2 * h] = mul2_rn(mul2_rn(add2_rn(make_float2(__uint_as_float(n[0]), __uint_as_float(n[1])), z01), f01), s2);
+                v[2 * h + 1] = mul2_rn(mul2_rn(add2_rn(make_float2(__uint_as_float(n[2]), __uint_as_float(n[3])), z23), f23), s2);
             }
-        } else {
+        }
+        T* const row = out + at.row * out_stride;
+        if (a.vec) {
+            if (!in) continue;
+            T* const o = row + c;
+            if (c + 8 <= cols) {
+                if constexpr (sizeof(T) == 4) {
+                    reinterpret_cast<float4*>(o)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+                    reinterpret_cast<float4*>(o)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+                } else {
+                    *reinterpret_cast<uint4*>(o) = make_uint4(pack_pair<T>(v[0].x, v[0].y), pack_pair<T>(v[1].x, v[1].y), pack_pair<T>(v[2].x, v[2].y), pack_pair<T>(v[3].x, v[3].y));
+                }
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (c + i < a.cols) o[i] = from_f32<T>(v[i]);
+                for (int i = 0; i < 8; ++i) if (c + i < cols) o[i] = from_f32<T>(i & 1 ? v[i / 2].y : v[i / 2].x);
+            }
+        } else {          // unaligned rows: neighbouring lanes write neighbouring elements
+            float* const mine = tmp[threadIdx.x >> 5];
+            if (in) {
+                reinterpret_cast<float4*>(mine)[2 * lane] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+                reinterpret_cast<float4*>(mine)[2 * lane + 1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c0 + i * 32 + lane < cols) row[c0 + i * 32 + lane] = from_f32<T>(mine[i * 32 + lane]);
+            __syncwarp();
         }
     }
 }
@@ -620,28 +782,48 @@ cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t 
 
 W4Quant pack_args(const W4Matrix& m, const void* w, int64_t stride, int es) {
     const bool vec = (reinterpret_cast<uintptr_t>(w) % 16 == 0) && (stride * es % 16 == 0);
-    return {w, stride, m.codes, m.scales, m.zeros, m.rows, m.cols, m.codes_stride, (m.cols + m.group - 1) / m.group, m.group, vec};
+    return {w, stride, m.codes, m.scales, m.zeros, m.rows, m.cols, m.codes_stride, (m.cols + m.group - 1) / m.group, m.group, vec, 0, 0, 0,
+            m.group == 32 ? 5 : m.group == 64 ? 6 : m.group == 128 ? 7 : -1, 1.0f};
+}
+
+// Lays `spans` spans per row out over the grid it returns: eight CTAs per SM, or as many as there is work for.
+int walk_spans(W4Quant& a, int64_t spans) {
+    const int64_t ctas = std::min<int64_t>((a.rows * spans + kW4Warps - 1) / kW4Warps, 148 * 8), warps = ctas * kW4Warps;
+    a.spans = (int)spans;
+    a.step_rows = (int)(warps / spans);
+    a.step_spans = (int)(warps % spans);
+    return (int)ctas;
 }
 
 }  // namespace
 
 cudaError_t launch_w4_quantize(const W4Matrix& m, const void* w, int dtype, int64_t w_stride, cudaStream_t s) {
-    const int64_t span = m.group > 128 ? m.group : 256;
-    const int grid = w4_grid((m.rows * ((m.cols + span - 1) / span) + 7) / 8);
     return with_dtype(dtype, [&](auto t) {
         return with_dtype(m.scale_dtype, [&](auto sc) {
-            w4_quantize_kernel<decltype(t), decltype(sc)><<<grid, kW4Threads, 0, s>>>(pack_args(m, w, w_stride, sizeof(t)));
+            using T = decltype(t);
+            using S = decltype(sc);
+            W4Quant a = pack_args(m, w, w_stride, sizeof(T));
+            if (m.group > 128) {
+                const int grid = walk_spans(a, a.groups);
+                w4_quantize_wide_kernel<T, S><<<grid, kW4Threads, 0, s>>>(a);
+            } else {
+                const int grid = walk_spans(a, (m.cols + kSpan - 1) / kSpan);
+                if (m.group == 32) w4_quantize_kernel<T, S, 4><<<grid, kW4Threads, 0, s>>>(a);
+                else if (m.group == 64) w4_quantize_kernel<T, S, 8><<<grid, kW4Threads, 0, s>>>(a);
+                else w4_quantize_kernel<T, S, 16><<<grid, kW4Threads, 0, s>>>(a);
+            }
             return cudaGetLastError();
         });
     });
 }
 
 cudaError_t launch_w4_dequantize(const W4Matrix& m, void* out, int dtype, int64_t out_stride, cudaStream_t s) {
-    const int grid = w4_grid((m.rows * ((m.cols + 7) / 8) + kW4Threads - 1) / kW4Threads);
     return with_dtype(dtype, [&](auto t) {
         return with_dtype(m.scale_dtype, [&](auto sc) {
             using T = decltype(t);
-            w4_dequantize_kernel<T, decltype(sc)><<<grid, kW4Threads, 0, s>>>(pack_args(m, out, out_stride, sizeof(T)), static_cast<T*>(out), out_stride);
+            W4Quant a = pack_args(m, out, out_stride, sizeof(T));
+            const int grid = walk_spans(a, (m.cols + kSpan - 1) / kSpan);
+            w4_dequantize_kernel<T, decltype(sc)><<<grid, kW4Threads, 0, s>>>(a, static_cast<T*>(out), out_stride);
             return cudaGetLastError();
         });
     });
