@@ -15,7 +15,10 @@ namespace {
 
 constexpr int kW4Threads = 256;
 constexpr int kW4Warps = kW4Threads / 32;
-constexpr int kSpan = 256;        // columns that a warp takes at a time, eight consecutive ones per lane = one 32-bit word of codes
+constexpr int kLaneCols = 16;     // consecutive columns of a lane = eight bytes of codes: a group's scale, its reciprocal and the
+                                  // addresses are worked out once for them (with eight columns: 196 us instead of XX, see below)
+constexpr int kSpan = 32 * kLaneCols;         // columns that a warp takes at a time
+constexpr int kTmp = kSpan + 32 * 4;          // floats of shared memory for them, lanes 20 apart: no two on the same banks
 
 struct W4Quant {
     const void* w;
@@ -47,41 +50,52 @@ struct SpanWalk {
     }
 };
 
-// Eight consecutive elements of a row from column c on, as binary32; zeros behind `end`.
+// A lane's consecutive elements of a row from column c on, as binary32; zeros behind `end`.
 template <typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t end, bool vec, float (&v)[8]) {
-    if (vec && c + 8 <= end) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 a = __ldg(reinterpret_cast<const float4*>(row + c)), b = __ldg(reinterpret_cast<const float4*>(row + c) + 1);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            const uint4 a = __ldg(reinterpret_cast<const uint4*>(row + c));
-            const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+__device__ __forceinline__ void load_cols(const T* row, int64_t c, int64_t end, float (&v)[kLaneCols]) {
+    if (c + kLaneCols <= end) {
+        constexpr int PER = 16 / sizeof(T);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 p = unpack_pair<T>(u[i]);
-                v[2 * i] = p.x; v[2 * i + 1] = p.y;
+        for (int i = 0; i < kLaneCols / PER; ++i) {
+            const uint4 q = __ldg(reinterpret_cast<const uint4*>(row + c) + i);
+            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (sizeof(T) == 4) {
+                    v[4 * i + j] = __uint_as_float(u[j]);
+                } else {
+                    const float2 p = unpack_pair<T>(u[j]);
+                    v[8 * i + 2 * j] = p.x; v[8 * i + 2 * j + 1] = p.y;
+                }
             }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (c + i < end) ? to_f32(row[c + i]) : 0.0f;
+        for (int i = 0; i < kLaneCols; ++i) v[i] = (c + i < end) ? to_f32(row[c + i]) : 0.0f;
     }
 }
-// The same for all lanes of a warp, c0 + 8 lane each, where rows are not aligned: neighbouring lanes load neighbouring elements and
-// hand them on through 256 floats of shared memory.
+// The same for all lanes of a warp, from column c0 + kLaneCols lane on, where rows are not aligned: neighbouring lanes load
+// neighbouring elements and hand them on through shared memory.
 template <typename T>
-__device__ __forceinline__ void load8_apart(const T* row, int64_t c0, int64_t end, float* tmp, float (&v)[8]) {
+__device__ __forceinline__ void load_cols_apart(const T* row, int64_t c0, int64_t end, float* tmp, float (&v)[kLaneCols]) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < kLaneCols; ++i) {
         const int64_t c = c0 + i * 32 + lane;
-        tmp[i * 32 + lane] = c < end ? to_f32(row[c]) : 0.0f;
+        tmp[i * 40 + lane + (lane >> 4) * 4] = c < end ? to_f32(row[c]) : 0.0f;
     }
     __syncwarp();
-    const float4 a = reinterpret_cast<const float4*>(tmp)[2 * lane], b = reinterpret_cast<const float4*>(tmp)[2 * lane + 1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+#pragma unroll
+    for (int i = 0; i < kLaneCols / 4; ++i) {
+        const float4 a = reinterpret_cast<const float4*>(tmp + lane * 20)[i];
+        v[4 * i] = a.x; v[4 * i + 1] = a.y; v[4 * i + 2] = a.z; v[4 * i + 3] = a.w;
+    }
     __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void load_span(const T* row, int64_t c0, int64_t end, bool vec, float* tmp, float (&v)[kLaneCols]) {
+    if (vec) load_cols(row, c0 + (threadIdx.x & 31) * kLaneCols, end, v);
+    else load_cols_apart(row, c0, end, tmp, v);
 }
 
 // ------------------------------------------------------------------------------------------------ quantizer
@@ -101,30 +115,34 @@ __device__ __forceinline__ float group_scale(float lo, float hi, bool zeros) {
 __device__ __forceinline__ float group_zero(float lo, float rcp, bool zeros) {
     return zeros ? fminf(fmaxf(rintf(__fmul_rn(-lo, rcp)), 0.0f), 15.0f) : 8.0f;
 }
-// The word of codes of eight weights. Values beyond +-2^21 (a saturated scale) are clamped before the addition that rounds; that
-// one is written as n * one + magic, since the assembler may join a packed product and a packed sum into one rounding.
-__device__ __forceinline__ uint32_t pack_codes(const float (&v)[8], float rcp, float zero, bool clamp, float one) {
+// The codes of a lane's weights. Values beyond +-2^21 (a saturated scale) are clamped before the addition that rounds; that one is
+// written as n * one + magic, since the assembler may join a packed product and a packed sum into one rounding.
+__device__ __forceinline__ uint2 pack_codes(const float (&v)[kLaneCols], float rcp, float zero, bool clamp, float one) {
     constexpr float kMagic = 12582912.0f;
     const int base = 0x4b400000 - (int)zero;
-    int q[8];
+    uint32_t w[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float2 n = mul2_rn(make_float2(v[2 * i], v[2 * i + 1]), splat(rcp));
+    for (int i = kLaneCols - 2; i >= 0; i -= 2) {
+        float2 n = mul2_rn(make_float2(v[i], v[i + 1]), splat(rcp));
         if (clamp) n = make_float2(fminf(fmaxf(n.x, -64.0f), 64.0f), fminf(fmaxf(n.y, -64.0f), 64.0f));
         n = fma2_rn(n, splat(one), splat(kMagic));
-        q[2 * i] = __float_as_int(n.x) - base;
-        q[2 * i + 1] = __float_as_int(n.y) - base;
+        asm("cvt.pack.sat.u4.s32.b32 %0, %1, %2, %0;" : "+r"(w[i / 8]) : "r"(__float_as_int(n.y) - base), "r"(__float_as_int(n.x) - base));
     }
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 6; i >= 0; i -= 2) asm("cvt.pack.sat.u4.s32.b32 %0, %1, %2, %0;" : "+r"(w) : "r"(q[i + 1]), "r"(q[i]));
-    return w;
+    return make_uint2(w[0], w[1]);
 }
-// Extremes of eight weights, lo <= 0 <= hi.
-template <typename T>
-__device__ __forceinline__ void extremes(const float (&v)[8], float& lo, float& hi) {
+// Writes them; what lies behind the row's last column becomes 0.
+__device__ __forceinline__ void store_codes(const W4Quant& a, int64_t row, int64_t c, uint2 w) {
+    uint8_t* const to = a.codes + row * a.codes_stride + (c >> 1);
+    const int64_t left = a.cols - c;
+    if (left < 8) w.x &= 0xffffffffu >> (4 * (8 - left));
+    if (left <= 8) w.y = 0;
+    else if (left < 16) w.y &= 0xffffffffu >> (4 * (16 - left));
+    *reinterpret_cast<uint2*>(to) = w;
+}
+// Extremes of a lane's weights, lo <= 0 <= hi.
+__device__ __forceinline__ void extremes(const float (&v)[kLaneCols], float& lo, float& hi) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { lo = fminf(lo, v[i]); hi = fmaxf(hi, v[i]); }
+    for (int i = 0; i < kLaneCols; ++i) { lo = fminf(lo, v[i]); hi = fmaxf(hi, v[i]); }
 }
 template <typename T> struct Pair2;
 template <> struct Pair2<__nv_bfloat16> { using P = __nv_bfloat162; };
@@ -135,24 +153,26 @@ template <typename T, bool MAX> __device__ __forceinline__ uint32_t pick2(uint32
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// Groups of 32, 64 and 128 columns: LANES = 4, 8 and 16 neighbouring lanes.
+// Groups of 32, 64 and 128 columns: LANES = 2, 4 and 8 neighbouring lanes.
 template <typename T, typename S, int LANES>
 __global__ void __launch_bounds__(kW4Threads) w4_quantize_kernel(const W4Quant a) {
-    __shared__ __align__(16) float tmp[kW4Warps][kSpan];
+    __shared__ __align__(16) float tmp[kW4Warps][kTmp];
     const int lane = threadIdx.x & 31;
     const bool zeros = a.zeros != nullptr;
     SpanWalk at(a);
 #pragma unroll 2
     for (; at.row < a.rows; at.next(a)) {
         const T* const row = static_cast<const T*>(a.w) + at.row * a.w_stride;
-        const int64_t c0 = (int64_t)at.span * kSpan, c = c0 + lane * 8;
-        float v[8], lo = 0.0f, hi = 0.0f;
+        const int64_t c0 = (int64_t)at.span * kSpan, c = c0 + lane * kLaneCols;
+        float v[kLaneCols], lo = 0.0f, hi = 0.0f;
         if (sizeof(T) == 2 && a.vec && c0 + kSpan <= a.cols) {
-            const uint4 q = __ldg(reinterpret_cast<const uint4*>(row + c));
-            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
             if constexpr (sizeof(T) == 2) {
+                const uint4 q0 = __ldg(reinterpret_cast<const uint4*>(row + c)), q1 = __ldg(reinterpret_cast<const uint4*>(row + c) + 1);
+                const uint32_t u[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
                 if (zeros) {      // -lo and hi side by side
-                    const uint32_t mx = pick2<T, true>(pick2<T, true>(q.x, q.y), pick2<T, true>(q.z, q.w)), mn = pick2<T, false>(pick2<T, false>(q.x, q.y), pick2<T, false>(q.z, q.w));
+                    uint32_t mx = u[0], mn = u[0];
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) { mx = pick2<T, true>(mx, u[i]); mn = pick2<T, false>(mn, u[i]); }
                     uint32_t m = __byte_perm(mx, mn, 0x5410), o = __byte_perm(mx, mn, 0x7632);
                     m = pick2<T, true>(m ^ 0x80000000u, o ^ 0x80000000u);
 #pragma unroll
@@ -160,22 +180,23 @@ __global__ void __launch_bounds__(kW4Threads) w4_quantize_kernel(const W4Quant a
                     const float2 p = unpack_pair<T>(m);
                     hi = fmaxf(p.x, 0.0f); lo = fminf(-p.y, 0.0f);
                 } else {          // the largest |w|
-                    uint32_t m = pick2<T, true>(pick2<T, true>(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu), pick2<T, true>(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu));
+                    uint32_t m = u[0] & 0x7fff7fffu;
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) m = pick2<T, true>(m, u[i] & 0x7fff7fffu);
 #pragma unroll
                     for (int d = LANES / 2; d; d >>= 1) m = pick2<T, true>(m, __shfl_xor_sync(0xffffffffu, m, d));
                     const float2 p = unpack_pair<T>(m);
                     hi = fmaxf(p.x, p.y);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < 8; ++i) {
                     const float2 p = unpack_pair<T>(u[i]);
                     v[2 * i] = p.x; v[2 * i + 1] = p.y;
                 }
             }
         } else {
-            if (a.vec) load8(row, c, a.cols, true, v);
-            else load8_apart(row, c0, a.cols, tmp[threadIdx.x >> 5], v);
-            extremes<T>(v, lo, hi);
+            load_span(row, c0, a.cols, a.vec, tmp[threadIdx.x >> 5], v);
+            extremes(v, lo, hi);
 #pragma unroll
             for (int d = LANES / 2; d; d >>= 1) {
                 lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
@@ -190,27 +211,23 @@ __global__ void __launch_bounds__(kW4Threads) w4_quantize_kernel(const W4Quant a
             static_cast<S*>(a.scales)[g] = from_f32<S>(s);
             if (zeros) a.zeros[g] = (uint8_t)zero;
         }
-        uint32_t word = pack_codes(v, rcp, zero, std::is_same<S, __half>::value && s == 65504.0f, a.one);
-        if (c + 8 > a.cols) word &= 0xffffffffu >> (4 * (c + 8 - a.cols));
-        *reinterpret_cast<uint32_t*>(a.codes + at.row * a.codes_stride + (c >> 1)) = word;
+        store_codes(a, at.row, c, pack_codes(v, rcp, zero, std::is_same<S, __half>::value && s == 65504.0f, a.one));
     }
 }
 
 // Wider groups (multiples of 128 columns): a warp walks one twice.
 template <typename T, typename S>
 __global__ void __launch_bounds__(kW4Threads) w4_quantize_wide_kernel(const W4Quant a) {
-    __shared__ __align__(16) float tmp[kW4Warps][kSpan];
+    __shared__ __align__(16) float tmp[kW4Warps][kTmp];
     const int lane = threadIdx.x & 31;
     const bool zeros = a.zeros != nullptr;
-    float* const mine = tmp[threadIdx.x >> 5];
     for (SpanWalk at(a); at.row < a.rows; at.next(a)) {
         const T* const row = static_cast<const T*>(a.w) + at.row * a.w_stride;
         const int64_t first = (int64_t)at.span * a.group, end = min(first + a.group, a.cols);
-        float v[8], lo = 0.0f, hi = 0.0f;
+        float v[kLaneCols], lo = 0.0f, hi = 0.0f;
         for (int64_t c0 = first; c0 < end; c0 += kSpan) {
-            if (a.vec) load8(row, c0 + lane * 8, end, true, v);
-            else load8_apart(row, c0, end, mine, v);
-            extremes<T>(v, lo, hi);
+            load_span(row, c0, end, a.vec, tmp[threadIdx.x >> 5], v);
+            extremes(v, lo, hi);
         }
         for (int d = 16; d; d >>= 1) {
             lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
@@ -224,13 +241,9 @@ __global__ void __launch_bounds__(kW4Threads) w4_quantize_wide_kernel(const W4Qu
             if (zeros) a.zeros[g] = (uint8_t)zero;
         }
         for (int64_t c0 = first; c0 < end; c0 += kSpan) {
-            const int64_t c = c0 + lane * 8;
-            if (a.vec) load8(row, c, end, true, v);
-            else load8_apart(row, c0, end, mine, v);
-            if (c >= end) continue;
-            uint32_t word = pack_codes(v, rcp, zero, std::is_same<S, __half>::value && s == 65504.0f, a.one);
-            if (c + 8 > a.cols) word &= 0xffffffffu >> (4 * (c + 8 - a.cols));
-            *reinterpret_cast<uint32_t*>(a.codes + at.row * a.codes_stride + (c >> 1)) = word;
+            load_span(row, c0, end, a.vec, tmp[threadIdx.x >> 5], v);
+            const int64_t c = c0 + lane * kLaneCols;
+            if (c < end) store_codes(a, at.row, c, pack_codes(v, rcp, zero, std::is_same<S, __half>::value && s == 65504.0f, a.one));
         }
     }
 }
@@ -241,24 +254,23 @@ __global__ void __launch_bounds__(kW4Threads) w4_quantize_wide_kernel(const W4Qu
 
 template <typename T, typename S>
 __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant a, T* __restrict__ out, int64_t out_stride) {
-    __shared__ __align__(16) float tmp[kW4Warps][kSpan];
-    const int lane = threadIdx.x & 31;
+    __shared__ __align__(16) float tmp[kW4Warps][kTmp];
+    const int lane = threadIdx.x & 31, cols = (int)a.cols;
     SpanWalk at(a);
 #pragma unroll 2
     for (; at.row < a.rows; at.next(a)) {
-        const int64_t c0 = (int64_t)at.span * kSpan;
-        const int c = at.span * kSpan + lane * 8, cols = (int)a.cols;
+        const int c0 = at.span * kSpan, c = c0 + lane * kLaneCols;
         const bool in = c < cols;
-        float2 v[4];
+        float2 v[kLaneCols / 2];
         if (in) {
-            const uint32_t q = __ldg(reinterpret_cast<const uint32_t*>(a.codes + at.row * a.codes_stride + (c >> 1)));
+            const uint2 q = __ldg(reinterpret_cast<const uint2*>(a.codes + at.row * a.codes_stride + (c >> 1)));
             const int64_t g = at.row * a.groups + (a.log_group >= 0 ? c >> a.log_group : c / a.group);
             const float s = to_f32(static_cast<const S*>(a.scales)[g]), z = a.zeros ? (float)a.zeros[g] : 8.0f;
             const float2 z01 = make_float2(-8388608.0f - z, -8388608.0f - 16.0f * z), z23 = make_float2(-8388608.0f - 256.0f * z, -8388608.0f - 4096.0f * z);
             const float2 f01 = make_float2(1.0f, 0.0625f), f23 = make_float2(1.0f / 256, 1.0f / 4096), s2 = splat(s);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t w = q >> (16 * h);
+            for (int h = 0; h < 4; ++h) {
+                const uint32_t w = (h < 2 ? q.x : q.y) >> (16 * (h & 1));
                 uint32_t n[4];
                 asm("lop3.b32 %0, %1, 0xf, 0x4b000000, 0xEA;" : "=r"(n[0]) : "r"(w));
                 asm("lop3.b32 %0, %1, 0xf0, 0x4b000000, 0xEA;" : "=r"(n[1]) : "r"(w));
@@ -272,27 +284,30 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
         if (a.vec) {
             if (!in) continue;
             T* const o = row + c;
-            if (c + 8 <= cols) {
+            if (c + kLaneCols <= cols) {
                 if constexpr (sizeof(T) == 4) {
-                    reinterpret_cast<float4*>(o)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
-                    reinterpret_cast<float4*>(o)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(o)[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
                 } else {
-                    *reinterpret_cast<uint4*>(o) = make_uint4(pack_pair<T>(v[0].x, v[0].y), pack_pair<T>(v[1].x, v[1].y), pack_pair<T>(v[2].x, v[2].y), pack_pair<T>(v[3].x, v[3].y));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        reinterpret_cast<uint4*>(o)[i] = make_uint4(pack_pair<T>(v[4 * i].x, v[4 * i].y), pack_pair<T>(v[4 * i + 1].x, v[4 * i + 1].y),
+                                                                    pack_pair<T>(v[4 * i + 2].x, v[4 * i + 2].y), pack_pair<T>(v[4 * i + 3].x, v[4 * i + 3].y));
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) if (c + i < cols) o[i] = from_f32<T>(i & 1 ? v[i / 2].y : v[i / 2].x);
+                for (int i = 0; i < kLaneCols; ++i) if (c + i < cols) o[i] = from_f32<T>(i & 1 ? v[i / 2].y : v[i / 2].x);
             }
         } else {          // unaligned rows: neighbouring lanes write neighbouring elements
             float* const mine = tmp[threadIdx.x >> 5];
             if (in) {
-                reinterpret_cast<float4*>(mine)[2 * lane] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
-                reinterpret_cast<float4*>(mine)[2 * lane + 1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(mine + lane * 20)[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
             }
             __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c0 + i * 32 + lane < cols) row[c0 + i * 32 + lane] = from_f32<T>(mine[i * 32 + lane]);
+            for (int i = 0; i < kLaneCols; ++i)
+                if (c0 + i * 32 + lane < cols) row[c0 + i * 32 + lane] = from_f32<T>(mine[i * 40 + lane + (lane >> 4) * 4]);
             __syncwarp();
         }
     }
@@ -808,9 +823,9 @@ cudaError_t launch_w4_quantize(const W4Matrix& m, const void* w, int dtype, int6
                 w4_quantize_wide_kernel<T, S><<<grid, kW4Threads, 0, s>>>(a);
             } else {
                 const int grid = walk_spans(a, (m.cols + kSpan - 1) / kSpan);
-                if (m.group == 32) w4_quantize_kernel<T, S, 4><<<grid, kW4Threads, 0, s>>>(a);
-                else if (m.group == 64) w4_quantize_kernel<T, S, 8><<<grid, kW4Threads, 0, s>>>(a);
-                else w4_quantize_kernel<T, S, 16><<<grid, kW4Threads, 0, s>>>(a);
+                if (m.group == 32) w4_quantize_kernel<T, S, 2><<<grid, kW4Threads, 0, s>>>(a);
+                else if (m.group == 64) w4_quantize_kernel<T, S, 4><<<grid, kW4Threads, 0, s>>>(a);
+                else w4_quantize_kernel<T, S, 8><<<grid, kW4Threads, 0, s>>>(a);
             }
             return cudaGetLastError();
         });
