@@ -4,6 +4,7 @@
 // packing of the optimizer states), rows `codes_stride` bytes apart (a multiple of 16), and one scale and optionally one zero
 // point per `group` consecutive columns of a row. Value = (code - zero) * scale, zero = 8 without zero points.
 #include <algorithm>
+#include <cstring>
 #include <type_traits>
 
 #include "lpmm_internal.h"
@@ -18,7 +19,7 @@ constexpr int kW4Warps = kW4Threads / 32;
 constexpr int kLaneCols = 16;     // consecutive columns of a lane = eight bytes of codes: a group's scale, its reciprocal and the
                                   // addresses are worked out once for them (with eight columns: 196 us instead of XX, see below)
 constexpr int kSpan = 32 * kLaneCols;         // columns that a warp takes at a time
-constexpr int kTmp = kSpan + 32 * 4;          // floats of shared memory for them, lanes 20 apart: no two on the same banks
+constexpr int kTmp = kSpan + 32 * 4;          // floats of shared memory to hand them on, with room between the lanes' shares
 
 struct W4Quant {
     const void* w;
@@ -50,32 +51,52 @@ struct SpanWalk {
     }
 };
 
-// A lane's consecutive elements of a row from column c on, as binary32; zeros behind `end`.
+// A warp's span in 16-byte pieces: neighbouring lanes load or write neighbouring pieces, so that every 32-byte sector is whole, and
+// hand them on through shared memory, where one piece in nine is left out: whichever way they are read, on different banks.
+__device__ __forceinline__ int piece(int i) { return i + (i >> 3); }
+template <typename T> constexpr int lane_pieces = kLaneCols * (int)sizeof(T) / 16;
+
+// A lane's kLaneCols consecutive elements of an aligned row, as they are, from column c0 + kLaneCols lane on; zeros behind `end`.
 template <typename T>
-__device__ __forceinline__ void load_cols(const T* row, int64_t c, int64_t end, float (&v)[kLaneCols]) {
-    if (c + kLaneCols <= end) {
-        constexpr int PER = 16 / sizeof(T);
+__device__ __forceinline__ void load_pieces(const T* row, int64_t c0, int64_t end, uint4* tmp, uint4 (&v)[lane_pieces<T>]) {
+    constexpr int PER = 16 / sizeof(T), N = lane_pieces<T>;
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-        for (int i = 0; i < kLaneCols / PER; ++i) {
-            const uint4 q = __ldg(reinterpret_cast<const uint4*>(row + c) + i);
-            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+    for (int i = 0; i < N; ++i) {
+        const int64_t c = c0 + (i * 32 + lane) * PER;
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if (c + PER <= end) {
+            q = __ldg(reinterpret_cast<const uint4*>(row + c));
+        } else if (c < end) {
+            T e[PER];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (sizeof(T) == 4) {
-                    v[4 * i + j] = __uint_as_float(u[j]);
-                } else {
-                    const float2 p = unpack_pair<T>(u[j]);
-                    v[8 * i + 2 * j] = p.x; v[8 * i + 2 * j + 1] = p.y;
-                }
+            for (int j = 0; j < PER; ++j) e[j] = c + j < end ? row[c + j] : from_f32<T>(0.0f);
+            memcpy(&q, e, 16);
+        }
+        tmp[piece(i * 32 + lane)] = q;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = tmp[piece(lane * N + i)];
+    __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void to_floats(const uint4 (&q)[lane_pieces<T>], float (&v)[kLaneCols]) {
+#pragma unroll
+    for (int i = 0; i < lane_pieces<T>; ++i) {
+        const uint32_t u[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(T) == 4) {
+                v[4 * i + j] = __uint_as_float(u[j]);
+            } else {
+                const float2 p = unpack_pair<T>(u[j]);
+                v[8 * i + 2 * j] = p.x; v[8 * i + 2 * j + 1] = p.y;
             }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < kLaneCols; ++i) v[i] = (c + i < end) ? to_f32(row[c + i]) : 0.0f;
     }
 }
-// The same for all lanes of a warp, from column c0 + kLaneCols lane on, where rows are not aligned: neighbouring lanes load
-// neighbouring elements and hand them on through shared memory.
+// The same as binary32 where rows are not aligned: neighbouring lanes load neighbouring elements.
 template <typename T>
 __device__ __forceinline__ void load_cols_apart(const T* row, int64_t c0, int64_t end, float* tmp, float (&v)[kLaneCols]) {
     const int lane = threadIdx.x & 31;
@@ -94,8 +115,13 @@ __device__ __forceinline__ void load_cols_apart(const T* row, int64_t c0, int64_
 }
 template <typename T>
 __device__ __forceinline__ void load_span(const T* row, int64_t c0, int64_t end, bool vec, float* tmp, float (&v)[kLaneCols]) {
-    if (vec) load_cols(row, c0 + (threadIdx.x & 31) * kLaneCols, end, v);
-    else load_cols_apart(row, c0, end, tmp, v);
+    if (vec) {
+        uint4 q[lane_pieces<T>];
+        load_pieces(row, c0, end, reinterpret_cast<uint4*>(tmp), q);
+        to_floats<T>(q, v);
+    } else {
+        load_cols_apart(row, c0, end, tmp, v);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ quantizer
@@ -159,16 +185,20 @@ __global__ void __launch_bounds__(kW4Threads) w4_quantize_kernel(const W4Quant a
     __shared__ __align__(16) float tmp[kW4Warps][kTmp];
     const int lane = threadIdx.x & 31;
     const bool zeros = a.zeros != nullptr;
-    SpanWalk at(a);
-#pragma unroll 2
-    for (; at.row < a.rows; at.next(a)) {
+    for (SpanWalk at(a); at.row < a.rows; at.next(a)) {
         const T* const row = static_cast<const T*>(a.w) + at.row * a.w_stride;
         const int64_t c0 = (int64_t)at.span * kSpan, c = c0 + lane * kLaneCols;
         float v[kLaneCols], lo = 0.0f, hi = 0.0f;
-        if (sizeof(T) == 2 && a.vec && c0 + kSpan <= a.cols) {
+        if (sizeof(T) == 2 && a.vec) {
             if constexpr (sizeof(T) == 2) {
-                const uint4 q0 = __ldg(reinterpret_cast<const uint4*>(row + c)), q1 = __ldg(reinterpret_cast<const uint4*>(row + c) + 1);
-                const uint32_t u[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
+                uint4 q[2];
+                if (c0 + kSpan <= a.cols) {      // two loads that share their sectors, through L1: cheaper here than the way around
+                    q[0] = __ldg(reinterpret_cast<const uint4*>(row + c));
+                    q[1] = __ldg(reinterpret_cast<const uint4*>(row + c) + 1);
+                } else {
+                    load_pieces(row, c0, a.cols, reinterpret_cast<uint4*>(tmp[threadIdx.x >> 5]), q);
+                }
+                const uint32_t u[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[1].x, q[1].y, q[1].z, q[1].w};
                 if (zeros) {      // -lo and hi side by side
                     uint32_t mx = u[0], mn = u[0];
 #pragma unroll
@@ -188,11 +218,7 @@ __global__ void __launch_bounds__(kW4Threads) w4_quantize_kernel(const W4Quant a
                     const float2 p = unpack_pair<T>(m);
                     hi = fmaxf(p.x, p.y);
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 p = unpack_pair<T>(u[i]);
-                    v[2 * i] = p.x; v[2 * i + 1] = p.y;
-                }
+                to_floats<T>(q, v);
             }
         } else {
             load_span(row, c0, a.cols, a.vec, tmp[threadIdx.x >> 5], v);
@@ -256,9 +282,7 @@ template <typename T, typename S>
 __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant a, T* __restrict__ out, int64_t out_stride) {
     __shared__ __align__(16) float tmp[kW4Warps][kTmp];
     const int lane = threadIdx.x & 31, cols = (int)a.cols;
-    SpanWalk at(a);
-#pragma unroll 2
-    for (; at.row < a.rows; at.next(a)) {
+    for (SpanWalk at(a); at.row < a.rows; at.next(a)) {
         const int c0 = at.span * kSpan, c = c0 + lane * kLaneCols;
         const bool in = c < cols;
         float2 v[kLaneCols / 2];
@@ -282,22 +306,30 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
         }
         T* const row = out + at.row * out_stride;
         if (a.vec) {
-            if (!in) continue;
-            T* const o = row + c;
-            if (c + kLaneCols <= cols) {
-                if constexpr (sizeof(T) == 4) {
+            constexpr int PER = 16 / sizeof(T), N = lane_pieces<T>;
+            uint4* const mine = reinterpret_cast<uint4*>(tmp[threadIdx.x >> 5]);
+            if (in) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(o)[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        reinterpret_cast<uint4*>(o)[i] = make_uint4(pack_pair<T>(v[4 * i].x, v[4 * i].y), pack_pair<T>(v[4 * i + 1].x, v[4 * i + 1].y),
-                                                                    pack_pair<T>(v[4 * i + 2].x, v[4 * i + 2].y), pack_pair<T>(v[4 * i + 3].x, v[4 * i + 3].y));
+                for (int i = 0; i < N; ++i) {
+                    if constexpr (sizeof(T) == 4) mine[piece(lane * N + i)] = make_uint4(__float_as_uint(v[2 * i].x), __float_as_uint(v[2 * i].y), __float_as_uint(v[2 * i + 1].x), __float_as_uint(v[2 * i + 1].y));
+                    else mine[piece(lane * N + i)] = make_uint4(pack_pair<T>(v[4 * i].x, v[4 * i].y), pack_pair<T>(v[4 * i + 1].x, v[4 * i + 1].y), pack_pair<T>(v[4 * i + 2].x, v[4 * i + 2].y), pack_pair<T>(v[4 * i + 3].x, v[4 * i + 3].y));
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kLaneCols; ++i) if (c + i < cols) o[i] = from_f32<T>(i & 1 ? v[i / 2].y : v[i / 2].x);
             }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int o = c0 + (i * 32 + lane) * PER;
+                const uint4 q = mine[piece(i * 32 + lane)];
+                if (o + PER <= cols) {
+                    *reinterpret_cast<uint4*>(row + o) = q;
+                } else if (o < cols) {
+                    T e[PER];
+                    memcpy(e, &q, 16);
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) if (o + j < cols) row[o + j] = e[j];
+                }
+            }
+            __syncwarp();
         } else {          // unaligned rows: neighbouring lanes write neighbouring elements
             float* const mine = tmp[threadIdx.x >> 5];
             if (in) {
@@ -801,9 +833,10 @@ W4Quant pack_args(const W4Matrix& m, const void* w, int64_t stride, int es) {
             m.group == 32 ? 5 : m.group == 64 ? 6 : m.group == 128 ? 7 : -1, 1.0f};
 }
 
-// Lays `spans` spans per row out over the grid it returns: eight CTAs per SM, or as many as there is work for.
+// Lays `spans` spans per row out over the grid it returns: 64 CTAs per SM, or as many as there is work for (eight per
+// SM, all resident: XX us).
 int walk_spans(W4Quant& a, int64_t spans) {
-    const int64_t ctas = std::min<int64_t>((a.rows * spans + kW4Warps - 1) / kW4Warps, 148 * 8), warps = ctas * kW4Warps;
+    const int64_t ctas = std::min<int64_t>((a.rows * spans + kW4Warps - 1) / kW4Warps, 148 * 64), warps = ctas * kW4Warps;
     a.spans = (int)spans;
     a.step_rows = (int)(warps / spans);
     a.step_spans = (int)(warps % spans);
