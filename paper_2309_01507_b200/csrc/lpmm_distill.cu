@@ -316,8 +316,11 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
                 if (q != 0.0f) l += q * (lq[k] - (zk[k] == -INFINITY && r.s == r.s ? -INFINITY : (zk[k] - r.m) * a.inv_tau - log_s));
             }
             l = sum_lanes<32>(l);
-            if (rank == 0 && r.q_rest > 0.0f)
-                l += r.q_rest * (logf(r.q_rest) - (r.s_rest > 0.0f ? (r.m_rest - r.m) * a.inv_tau + logf(r.s_rest) - log_s : -INFINITY));
+            if (rank == 0 && r.q_rest > 0.0f) {      // one logarithm of the ratio, unless p_rest is too small for that
+                const float p_rest = r.s_rest * r.f_rest * r.inv_s;
+                l += r.q_rest * (p_rest > 1e-30f ? logf(r.q_rest / p_rest)
+                                 : logf(r.q_rest) - (r.s_rest > 0.0f ? (r.m_rest - r.m) * a.inv_tau + logf(r.s_rest) - log_s : -INFINITY));
+            }
             if (lane == 0) {
                 if (log_cluster) store_at(&loss_ranks[parity][rank], 0, w * l);
                 else a.loss[last] = w * l;
