@@ -20,7 +20,8 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxCluster = 8;
-constexpr int blocks_per_sm(int threads) { return 1024 / threads; }
+constexpr size_t kRowRoom = 227 * 1024 - 4096;     // shared memory for a slice and what goes with it
+template <int THREADS> constexpr int ctas_per_sm = 1024 / THREADS;      // by their registers
 
 __device__ __forceinline__ float ex2(float x) {
     float r;
@@ -139,24 +140,34 @@ template <typename T> struct Slice {
     }
 };
 
-// The first row from t on, in steps of `step`, that has a weight. weight_at() is asked 32 rows ahead, one per lane.
-__device__ __forceinline__ float weight_ahead(const DistillArgs& a, int64_t t, int64_t step) {
-    const int64_t i = t + (threadIdx.x & 31) * step;
-    return i < a.tokens && a.weights ? a.weights[i] : 1.0f;
-}
-__device__ __forceinline__ int64_t live_row(const DistillArgs& a, int64_t t, int64_t step, float ahead) {
-    for (;;) {
-        const uint32_t live = __ballot_sync(0xffffffffu, ahead != 0.0f);
-        if (live) return min(t + (__ffs(live) - 1) * step, a.tokens);
-        t += 32 * step;
-        ahead = weight_ahead(a, t, step);
+// The n-th row behind row t that has a weight (a.tokens if there is none), found by a whole warp, 256 rows at a time: the rows
+// without one cost no CTA its turn.
+__device__ __forceinline__ int64_t live_row(const DistillArgs& a, int64_t t, int n) {
+    if (!a.weights) return min(t + n, a.tokens);
+    const int lane = threadIdx.x & 31;
+    for (int64_t base = t + 1; base < a.tokens; base += 256) {
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = base + i * 32 + lane < a.tokens ? a.weights[base + i * 32 + lane] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t live = __ballot_sync(0xffffffffu, w[i] != 0.0f);
+            if (__popc(live) >= n) {
+                const uint32_t it = __ballot_sync(0xffffffffu, (live >> lane & 1) && __popc(live & ((2u << lane) - 1)) == n);
+                return base + i * 32 + __ffs(it) - 1;
+            }
+            n -= __popc(live);
+        }
     }
+    return a.tokens;
 }
 
-// Named barriers between the workers and the teacher's warp; "arrive" does not wait.
+// Named barriers between the workers and the teacher's warp; "pass" does not wait.
 enum { B_ROW = 1, B_TAKEN, B_PARTS, B_PARTS_SEEN, B_WRITTEN };
-template <int THREADS> __device__ __forceinline__ void meet(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(THREADS + 32) : "memory"); }
-template <int THREADS> __device__ __forceinline__ void pass(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(THREADS + 32) : "memory"); }
+template <int THREADS> struct Barriers {
+    __device__ __forceinline__ static void meet(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(THREADS + 32) : "memory"); }
+    __device__ __forceinline__ static void pass(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(THREADS + 32) : "memory"); }
+};
 
 // What the classes of a row come to.
 struct RowSums {
@@ -178,8 +189,9 @@ struct RowSums {
 // entries: it prepares their q a row ahead, takes them out of the slice (sets them to -infinity), adds up the loss and writes
 // their gradients over the workers'.
 template <typename T, int THREADS, bool GRAD>
-__global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_kernel(const DistillArgs a, const int log_cluster, const int slice_vecs) {
+__global__ void __launch_bounds__(THREADS + 32, ctas_per_sm<THREADS>) distill_kernel(const DistillArgs a, const int log_cluster, const int slice_vecs) {
     constexpr int VE = Row<T>::n, WARPS = THREADS / 32;
+    using bar = Barriers<THREADS>;
     extern __shared__ __align__(16) unsigned char smem[];
     uint4* const vec = reinterpret_cast<uint4*>(smem);
     T* const elem = reinterpret_cast<T*>(smem);
@@ -190,13 +202,14 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
     uint32_t* const bits = reinterpret_cast<uint32_t*>(zk + K);          // one per element, to find ids that are listed twice
     __shared__ float part[WARPS][2], top_part[3], teacher[2];
     __shared__ float ranks[2][kMaxCluster][5], loss_ranks[2][kMaxCluster];
+    __shared__ int next_row;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, V = (int)a.vocab;
     const int cluster = 1 << log_cluster, rank = log_cluster ? (int)cluster_rank() : 0;
     const float c = a.inv_tau * kLog2e;
     const bool tail = a.teacher_lse != nullptr;
-    const int64_t step = gridDim.x >> log_cluster, first_row = blockIdx.x >> log_cluster;
+    const int step = gridDim.x >> log_cluster, first_row = blockIdx.x >> log_cluster;
     if (log_cluster) cluster_barrier();       // every CTA is there before another stores into its shared memory
-    int64_t t = live_row(a, first_row, step, weight_ahead(a, first_row, step));
+    int64_t t = live_row(a, -1, first_row + 1);       // the rows with a weight, in turn
     int parity = 0;
     // The row's classes over the whole cluster, from the ranks' parts.
     const auto joined = [&](float2& rest, float2& top, float& n_top) {
@@ -259,6 +272,7 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
             __syncwarp();
         };
         if (t < a.tokens) prepare(t, 0);
+        int64_t next = t < a.tokens ? live_row(a, t, step) : t;
         while (t < a.tokens) {
             const int* const slot = slots + parity * K;
             const float* const lq = lqs + parity * K;
@@ -266,16 +280,15 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
             const bool twice = twice_next;
             const Slice<T> sl(a, t, rank, log_cluster);
             T* const g = GRAD ? static_cast<T*>(a.grad) + t * a.grad_stride + sl.e0 : nullptr;
-            const float ahead = weight_ahead(a, t + step, step);
-            if (lane == 0) { teacher[0] = s_t; teacher[1] = w; }
-            meet<THREADS>(B_ROW);
+            if (lane == 0) { teacher[0] = s_t; teacher[1] = w; next_row = (int)next; }
+            bar::meet(B_ROW);
             float m_top = -INFINITY, s_top = 0.0f, n_top = 0.0f;
             for (int k = lane; k < K; k += 32)
                 if (const int e = slot[k]; e >= 0) m_top = fmaxf(m_top, zk[k] = to_f32(elem[e]));
             __syncwarp();
             for (int k = lane; k < K; k += 32)
                 if (const int e = slot[k]; e >= 0) reinterpret_cast<typename Row<T>::Bits*>(elem)[e] = Row<T>::minus_inf;
-            pass<THREADS>(B_TAKEN);
+            bar::pass(B_TAKEN);
             m_top = warp_max1(m_top);
             for (int k = lane; k < K; k += 32) {
                 const int e = slot[k];
@@ -290,10 +303,10 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
             s_top = sum_lanes<32>(s_top);
             n_top = sum_lanes<32>(n_top);
             if (lane == 0) { top_part[0] = m_top; top_part[1] = s_top; top_part[2] = n_top; }
-            pass<THREADS>(B_PARTS);
+            bar::pass(B_PARTS);
             if (log_cluster) cluster_arrive();
             last = t;
-            t = live_row(a, t + step, step, ahead);
+            t = next;
             if (t < a.tokens) prepare(t, parity ^ 1);
             float2 rest, top;
             if (log_cluster) {
@@ -304,7 +317,7 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
                 }
                 joined(rest, top, n_top);
             } else {
-                meet<THREADS>(B_PARTS_SEEN);
+                bar::meet(B_PARTS_SEEN);
                 own_classes(rest, top, n_top);
             }
             const RowSums r(rest, top, n_top, s_t, c, tail, V);
@@ -337,11 +350,12 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
                     }
                     zk[k] = __fmaf_rn(ex2((zk[k] - r.m) * c), q_scale, -q * scale);
                 }
-                meet<THREADS>(B_WRITTEN);
+                bar::meet(B_WRITTEN);
                 for (int k = lane; k < K; k += 32) if (const int e = slot[k]; e >= 0) g[e] = from_f32<T>(zk[k]);
             }
             before = last;
             parity ^= 1;
+            if (t < a.tokens) next = live_row(a, t, step);
         }
         if (log_cluster) {
             cluster_barrier();
@@ -357,18 +371,21 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
         const Slice<T> sl(a, t, rank, log_cluster);
         for (int v = tid; v < sl.nv; v += THREADS) sl.fetch(vec, v, V);
     }
-    if (a.weights) {                          // rows without a weight, while the first one arrives
-        for (int64_t r = first_row; r < a.tokens; r += step) {
-            if (a.weights[r] != 0.0f) continue;
-            if (rank == 0 && tid == 0) a.loss[r] = 0.0f;
-            if constexpr (GRAD) {
-                T* const g = static_cast<T*>(a.grad) + r * a.grad_stride;
-                const Slice<T> sl(a, r, rank, log_cluster);
-                const int j0 = min(sl.j1, sl.j0 + (int)((16 - reinterpret_cast<uintptr_t>(g + sl.j0) % 16) % 16 / sizeof(T)));
-                const int n = (sl.j1 - j0) / VE, j1 = j0 + n * VE;
-                if (tid < j0 - sl.j0) g[sl.j0 + tid] = from_f32<T>(0.0f);
-                if (tid < sl.j1 - j1) g[j1 + tid] = from_f32<T>(0.0f);
-                for (int v = tid; v < n; v += THREADS) reinterpret_cast<uint4*>(g + j0)[v] = make_uint4(0, 0, 0, 0);
+    if (a.weights) {                          // rows without a weight, while the first one arrives; 32 are looked at together
+        for (int64_t r0 = first_row; r0 < a.tokens; r0 += 32 * (int64_t)step) {
+            const int64_t mine = r0 + lane * (int64_t)step;
+            for (uint32_t dead = __ballot_sync(0xffffffffu, mine < a.tokens && a.weights[min(mine, a.tokens - 1)] == 0.0f); dead; dead &= dead - 1) {
+                const int64_t r = r0 + (__ffs(dead) - 1) * (int64_t)step;
+                if (rank == 0 && tid == 0) a.loss[r] = 0.0f;
+                if constexpr (GRAD) {
+                    T* const g = static_cast<T*>(a.grad) + r * a.grad_stride;
+                    const Slice<T> sl(a, r, rank, log_cluster);
+                    const int j0 = min(sl.j1, sl.j0 + (int)((16 - reinterpret_cast<uintptr_t>(g + sl.j0) % 16) % 16 / sizeof(T)));
+                    const int n = (sl.j1 - j0) / VE, j1 = j0 + n * VE;
+                    if (tid < j0 - sl.j0) g[sl.j0 + tid] = from_f32<T>(0.0f);
+                    if (tid < sl.j1 - j1) g[j1 + tid] = from_f32<T>(0.0f);
+                    for (int v = tid; v < n; v += THREADS) reinterpret_cast<uint4*>(g + j0)[v] = make_uint4(0, 0, 0, 0);
+                }
             }
         }
     }
@@ -376,12 +393,11 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
     while (t < a.tokens) {
         const Slice<T> sl(a, t, rank, log_cluster);
         const int nv = sl.nv;
-        const float ahead = weight_ahead(a, t + step, step);
         copies_landed();
-        meet<THREADS>(B_ROW);
+        bar::meet(B_ROW);
         const float s_t = teacher[0], w = teacher[1];
-        meet<THREADS>(B_TAKEN);
-        const int64_t t_next = live_row(a, t + step, step, ahead);
+        const int64_t t_next = next_row;
+        bar::meet(B_TAKEN);
         const Slice<T> next(a, min(t_next, a.tokens - 1), rank, log_cluster);
         const int nv_next = t_next < a.tokens ? next.nv : 0;
         const auto fetch_more = [&] {      // the next row may have a vector more than this one
@@ -409,8 +425,8 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
             const float s = sum_lanes<32>(sum.x + sum.y);
             if (lane == 0) { part[warp][0] = m; part[warp][1] = s; }
         }
-        meet<THREADS>(B_PARTS);
-        if (!log_cluster) pass<THREADS>(B_PARTS_SEEN);
+        bar::meet(B_PARTS);
+        if (!log_cluster) bar::pass(B_PARTS_SEEN);
         if (GRAD || log_cluster) {
             float2 rest, top;
             float n_top;
@@ -452,7 +468,7 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
                         }
                     }
                     fetch_more();
-                    pass<THREADS>(B_WRITTEN);
+                    bar::pass(B_WRITTEN);
                 } else {
                     // The gradient's rows are aligned otherwise than the logits': its own vectors, gathered element by element.
                     const int goff = (int)(reinterpret_cast<uintptr_t>(g) % 16 / sizeof(T));
@@ -474,7 +490,7 @@ __global__ void __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) distill_
                                 if (j + i >= sl.j0 && j + i < sl.j1) g[j + i] = from_f32<T>(i & 1 ? x[i / 2].y : x[i / 2].x);
                         }
                     }
-                    meet<THREADS>(B_WRITTEN);
+                    bar::meet(B_WRITTEN);
                     for (int v = tid; v < nv_next; v += THREADS) next.fetch(vec, v, V);
                 }
             }
@@ -491,8 +507,8 @@ cudaError_t launch(const DistillArgs& a, int log_cluster, int slice_vecs, size_t
     auto kernel = distill_kernel<T, THREADS, GRAD>;
     cudaError_t e = bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) : cudaSuccess;
     if (e != cudaSuccess) return e;
-    // As many CTAs as the SMs hold (their registers: see the launch bounds), each on every so manieth row.
-    const int per_sm = std::max(1, std::min(blocks_per_sm(THREADS), (int)(227 * 1024 / (bytes + 2048))));
+    // As many CTAs as the SMs hold, each on every so manieth row that has a weight.
+    const int per_sm = std::max(1, std::min(ctas_per_sm<THREADS>, (int)(227 * 1024 / (bytes + 2048))));
     const int64_t rows = std::min<int64_t>(a.tokens, (148 * per_sm) >> log_cluster);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * cluster));
@@ -517,10 +533,12 @@ cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, cudaStream_t 
     // A CTA takes a whole row where its shared memory holds one; the CTAs of a cluster wait for one another twice per row, which
     // costs more than it gains. Few rows are split, until every SM has a CTA or a slice is down to 8 KB.
     int log_cluster = 0;
-    while (log_cluster < 3 && row_vecs > (int64_t)12800 << log_cluster) ++log_cluster;
+    const auto slice_of = [&](int l) { return ((row_vecs + (1 << l) - 1) >> l) + 1; };
+    const auto bytes_of = [&](int l) { return (size_t)(slice_of(l) * 16 + a.top * 20 + (slice_of(l) * 16 / es + 31) / 32 * 4 + 15) / 16 * 16; };
+    while (log_cluster < 3 && bytes_of(log_cluster) > kRowRoom) ++log_cluster;
     while (log_cluster < 3 && a.tokens << log_cluster < 148 && row_vecs > (int64_t)1024 << log_cluster) ++log_cluster;
-    const int slice = (int)((row_vecs + (1 << log_cluster) - 1) >> log_cluster) + 1;
-    const size_t bytes = (size_t)slice * 16 + (size_t)a.top * 20 + ((size_t)slice * 16 / es + 31) / 32 * 4;
+    const int slice = (int)slice_of(log_cluster);
+    const size_t bytes = bytes_of(log_cluster);
     return with_dtype(logits_dtype, [&](auto t) {
         using T = decltype(t);
         if (slice <= 1024) return a.grad ? launch<T, 128, true>(a, log_cluster, slice, bytes, s) : launch<T, 128, false>(a, log_cluster, slice, bytes, s);

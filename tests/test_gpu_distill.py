@@ -124,6 +124,26 @@ def test_sizes_from_one_row_to_many(tokens, vocab, dtype):
     _check(z, ids, t, 2.0, lse, w, rows=sorted({0, tokens // 2, tokens - 1, min(5, tokens - 1)}))
 
 
+@pytest.mark.parametrize("vocab,top", [(50000, 1024), (52900, 1024), (53500, 700), (17300, 1024), (262144, 1024)])
+def test_the_longest_rows_that_fit_with_the_longest_lists(vocab, top):
+    for dtype in (F32, BF16):
+        for tokens in (2, 160):
+            z, ids, t, lse = _case(tokens, vocab, top, dtype, vocab, 1.0, True)
+            _check(z, ids, t, 1.0, lse, rows=[0, tokens - 1])
+
+
+def test_rows_without_a_weight_anywhere():
+    z, ids, t, lse = _case(1500, 700, 5, BF16, 77, 1.0, True)
+    for share in (0.0, 0.02, 0.5, 0.97, 1.0):
+        w = (torch.rand(1500, generator=torch.Generator("cuda").manual_seed(3), device="cuda") >= share).float() * 0.25
+        w[0], w[-1] = float(share == 0.5), float(share == 0.97)
+        z2 = torch.where(w[:, None] == 0, float("nan"), z.float()).to(BF16)      # rows that are not to be read
+        loss, grad = _check(z2, ids, t, 1.0, lse, w, rows=w.nonzero()[:, 0][:: max(1, int(w.count_nonzero()) // 40)].tolist())
+        assert (loss[w == 0] == 0).all() and (grad[w == 0] == 0).all() and torch.isfinite(loss).all()
+        base, gbase = lpmm.distill_grad(z, ids, t, teacher_lse=lse)
+        assert torch.equal(loss, torch.where(w == 0, 0.0, base * w))            # weights only scale
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
 def test_types_of_ids_and_teacher_strides_and_in_place(dtype):
     z, ids, t, lse = _case(6, 999, 20, dtype, 3, 1.0, True)
