@@ -464,6 +464,7 @@ def state_view_axis(state: State, tensor: int, axis: int) -> torch.Tensor:
 
 DISTILL_MAX_TOP, DISTILL_MAX_VOCAB = 1024, 262144
 _DTYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_IDS_BYTES = {torch.int32: 4, torch.int64: 8}
 
 
 class _elsewhere:
@@ -513,8 +514,10 @@ def _rows_of(x: torch.Tensor, name: str) -> int:
 
 
 def _dtype_of(x: torch.Tensor, name: str) -> int:
-    _need(x.dtype in _DTYPE, f"{name} must be float32, bfloat16 or float16, not {x.dtype}")
-    return _DTYPE[x.dtype]
+    d = _DTYPE.get(x.dtype)
+    if d is None:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, not {x.dtype}")
+    return d
 
 
 class W4Matrix:
@@ -616,34 +619,30 @@ def w4_matvec(m: W4Matrix, x: torch.Tensor, *, bias=None, out=None, out_dtype=No
 
 
 def _distill(logits, top_ids, top_logits, temperature, teacher_lse, weights, grad, stream):
-    _need(logits.is_cuda and logits.dim() == 2 and logits.shape[1] > 0, "logits must be a tokens x vocabulary CUDA tensor")
-    device = logits.device
+    device, shape, top = logits.device, logits.shape, top_ids.shape
+    _need(logits.is_cuda and len(shape) == 2 and shape[1] > 0, "logits must be a tokens x vocabulary CUDA tensor")
     if not _here(stream, device):
         with _elsewhere(stream, device, logits, top_ids, top_logits, teacher_lse, weights, grad if grad is not True else None):
             return _distill(logits, top_ids, top_logits, temperature, teacher_lse, weights, grad, None)
-    tokens, vocab = logits.shape
-    shape = top_ids.shape
-    if len(shape) != 2 or shape[0] != tokens or shape != top_logits.shape:
+    tokens, vocab = shape
+    if len(top) != 2 or top[0] != tokens or top != top_logits.shape:
         raise ValueError("top_ids and top_logits must be tokens x top")
-    ids_bytes = 8 if top_ids.dtype == torch.int64 else 4 if top_ids.dtype == torch.int32 else 0
+    ids_bytes = _IDS_BYTES.get(top_ids.dtype, 0)
     _need(ids_bytes, "top_ids must be int32 or int64")
-    lse = wts = None
     if not (top_ids.is_contiguous() and top_logits.is_contiguous() and top_ids.device == device and top_logits.device == device):
         raise ValueError("top_ids and top_logits must be contiguous and on the logits' device")
-    if teacher_lse is not None:
-        lse = _per_row(teacher_lse, "teacher_lse", tokens, device)
-    if weights is not None:
-        wts = _per_row(weights, "weights", tokens, device)
+    lse = None if teacher_lse is None else _per_row(teacher_lse, "teacher_lse", tokens, device)
+    wts = None if weights is None else _per_row(weights, "weights", tokens, device)
     loss = logits.new_empty(tokens, dtype=torch.float32)
     args = (logits.data_ptr(), _dtype_of(logits, "logits"), _rows_of(logits, "logits"), tokens, vocab, top_ids.data_ptr(), ids_bytes,
-            top_logits.data_ptr(), _dtype_of(top_logits, "top_logits"), shape[1], lse, wts, temperature, loss.data_ptr())
+            top_logits.data_ptr(), _dtype_of(top_logits, "top_logits"), top[1], lse, wts, temperature, loss.data_ptr())
     if grad is None:
         _check(lib().lpmm_distill_loss(*args, _raw_stream(device)), "lpmm_distill_loss")
         return loss, None
     if grad is True:
-        grad, stride = logits.new_empty((tokens, vocab)), vocab
+        grad, stride = logits.new_empty(shape), vocab
     else:
-        _need(grad.shape == logits.shape and grad.dtype == logits.dtype and grad.device == device, "out must match the logits")
+        _need(grad.shape == shape and grad.dtype == logits.dtype and grad.device == device, "out must match the logits")
         stride = _rows_of(grad, "out")
     _check(lib().lpmm_distill_grad(*args, grad.data_ptr(), stride, _raw_stream(device)), "lpmm_distill_grad")
     return loss, grad
