@@ -209,6 +209,7 @@ __global__ void __launch_bounds__(THREADS + 32, ctas_per_sm<THREADS>) distill_ke
     const bool tail = a.teacher_lse != nullptr;
     const int step = gridDim.x >> log_cluster, first_row = blockIdx.x >> log_cluster;
     if (log_cluster) cluster_barrier();       // every CTA is there before another stores into its shared memory
+    after_previous();
     int64_t t = live_row(a, -1, first_row + 1);       // the rows with a weight, in turn
     int parity = 0;
     // The row's classes over the whole cluster, from the ranks' parts.
@@ -503,26 +504,13 @@ __global__ void __launch_bounds__(THREADS + 32, ctas_per_sm<THREADS>) distill_ke
 
 template <typename T, int THREADS, bool GRAD>
 cudaError_t launch(const DistillArgs& a, int log_cluster, int slice_vecs, size_t bytes, cudaStream_t s) {
-    const int cluster = 1 << log_cluster;
     auto kernel = distill_kernel<T, THREADS, GRAD>;
     cudaError_t e = bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) : cudaSuccess;
     if (e != cudaSuccess) return e;
     // As many CTAs as the SMs hold, each on every so manieth row that has a weight.
     const int per_sm = std::max(1, std::min(ctas_per_sm<THREADS>, (int)(227 * 1024 / (bytes + 2048))));
     const int64_t rows = std::min<int64_t>(a.tokens, (148 * per_sm) >> log_cluster);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(rows * cluster));
-    cfg.blockDim = dim3(THREADS + 32);
-    cfg.dynamicSmemBytes = bytes;
-    cfg.stream = s;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = cluster;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = cluster > 1 ? 1 : 0;
-    e = cudaLaunchKernelEx(&cfg, kernel, a, log_cluster, slice_vecs);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    return launch_early(kernel, dim3((unsigned)(rows << log_cluster)), THREADS + 32, bytes, 1 << log_cluster, s, a, log_cluster, slice_vecs);
 }
 
 }  // namespace

@@ -50,4 +50,27 @@ cudaError_t with_dtype(int dtype, F&& f) {
     return f(__half{});
 }
 
+// Launches a kernel that begins with after_previous(): its CTAs may be set up while the work before it in the stream ends, which
+// saves about 2 us between two launches (32000 x 4096 product: 20.5 -> 18.8 us among others). cluster: CTAs per cluster.
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t shared, int cluster, cudaStream_t s, A&&... args) {
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<A&&>(args)...);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+// Waits until all that was in the stream before has ended and its writes can be seen. Nothing before it touches memory.
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 }  // namespace lpmm

@@ -185,6 +185,7 @@ __global__ void __launch_bounds__(kW4Threads) w4_quantize_kernel(const W4Quant a
     __shared__ __align__(16) float tmp[kW4Warps][kTmp];
     const int lane = threadIdx.x & 31;
     const bool zeros = a.zeros != nullptr;
+    after_previous();
     for (SpanWalk at(a); at.row < a.rows; at.next(a)) {
         const T* const row = static_cast<const T*>(a.w) + at.row * a.w_stride;
         const int64_t c0 = (int64_t)at.span * kSpan, c = c0 + lane * kLaneCols;
@@ -247,6 +248,7 @@ __global__ void __launch_bounds__(kW4Threads) w4_quantize_wide_kernel(const W4Qu
     __shared__ __align__(16) float tmp[kW4Warps][kTmp];
     const int lane = threadIdx.x & 31;
     const bool zeros = a.zeros != nullptr;
+    after_previous();
     for (SpanWalk at(a); at.row < a.rows; at.next(a)) {
         const T* const row = static_cast<const T*>(a.w) + at.row * a.w_stride;
         const int64_t first = (int64_t)at.span * a.group, end = min(first + a.group, a.cols);
@@ -282,6 +284,7 @@ template <typename T, typename S>
 __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant a, T* __restrict__ out, int64_t out_stride) {
     __shared__ __align__(16) float tmp[kW4Warps][kTmp];
     const int lane = threadIdx.x & 31, cols = (int)a.cols;
+    after_previous();
     for (SpanWalk at(a); at.row < a.rows; at.next(a)) {
         const int c0 = at.span * kSpan, c = c0 + lane * kLaneCols;
         const bool in = c < cols;
@@ -628,6 +631,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4P
             }
         }
     };
+    after_previous();
     load_x();
     float sa[NS], sb[NS], za[NS], zb[NS];
     if (u0 < u1) load_scales(sa, sb, za, zb);
@@ -812,19 +816,7 @@ cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t 
     auto kernel = w4_product_kernel<T, NT, GB>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.bytes);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(plan.clusters * plan.ranks), (unsigned)blocks);
-    cfg.blockDim = dim3(plan.warps * 32);
-    cfg.dynamicSmemBytes = plan.bytes;
-    cfg.stream = s;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = plan.ranks;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = plan.ranks > 1 ? 1 : 0;
-    e = cudaLaunchKernelEx(&cfg, kernel, p);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    return launch_early(kernel, dim3((unsigned)(plan.clusters * plan.ranks), (unsigned)blocks), plan.warps * 32, plan.bytes, plan.ranks, s, p);
 }
 
 W4Quant pack_args(const W4Matrix& m, const void* w, int64_t stride, int es) {
@@ -853,14 +845,12 @@ cudaError_t launch_w4_quantize(const W4Matrix& m, const void* w, int dtype, int6
             W4Quant a = pack_args(m, w, w_stride, sizeof(T));
             if (m.group > 128) {
                 const int grid = walk_spans(a, a.groups);
-                w4_quantize_wide_kernel<T, S><<<grid, kW4Threads, 0, s>>>(a);
-            } else {
-                const int grid = walk_spans(a, (m.cols + kSpan - 1) / kSpan);
-                if (m.group == 32) w4_quantize_kernel<T, S, 2><<<grid, kW4Threads, 0, s>>>(a);
-                else if (m.group == 64) w4_quantize_kernel<T, S, 4><<<grid, kW4Threads, 0, s>>>(a);
-                else w4_quantize_kernel<T, S, 8><<<grid, kW4Threads, 0, s>>>(a);
+                return launch_early(w4_quantize_wide_kernel<T, S>, dim3(grid), kW4Threads, 0, 1, s, a);
             }
-            return cudaGetLastError();
+            const int grid = walk_spans(a, (m.cols + kSpan - 1) / kSpan);
+            if (m.group == 32) return launch_early(w4_quantize_kernel<T, S, 2>, dim3(grid), kW4Threads, 0, 1, s, a);
+            if (m.group == 64) return launch_early(w4_quantize_kernel<T, S, 4>, dim3(grid), kW4Threads, 0, 1, s, a);
+            return launch_early(w4_quantize_kernel<T, S, 8>, dim3(grid), kW4Threads, 0, 1, s, a);
         });
     });
 }
@@ -871,8 +861,7 @@ cudaError_t launch_w4_dequantize(const W4Matrix& m, void* out, int dtype, int64_
             using T = decltype(t);
             W4Quant a = pack_args(m, out, out_stride, sizeof(T));
             const int grid = walk_spans(a, (m.cols + kSpan - 1) / kSpan);
-            w4_dequantize_kernel<T, decltype(sc)><<<grid, kW4Threads, 0, s>>>(a, static_cast<T*>(out), out_stride);
-            return cudaGetLastError();
+            return launch_early(w4_dequantize_kernel<T, decltype(sc)>, dim3(grid), kW4Threads, 0, 1, s, a, static_cast<T*>(out), out_stride);
         });
     });
 }

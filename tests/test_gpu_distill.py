@@ -258,3 +258,25 @@ def test_rows_beyond_2_31_elements_and_another_stream():
     for part in (slice(0, 3), slice(tokens - 3, tokens)):
         l2, g2 = _check(z[part].clone(), ids[part].clone(), t[part].clone(), rows=[0, 2])
         assert torch.allclose(l2, loss[part], rtol=1e-5, atol=1e-5) and torch.allclose(g2.float(), grad[part].float(), rtol=2.0 ** -7, atol=1e-7)
+
+
+def test_in_a_graph_between_other_work():
+    """Captured between kernels that produce its inputs and consume its outputs, and replayed with new values in the same buffers."""
+    z, ids, t, lse = _case(64, 5001, 12, BF16, 51, 1.0, True)
+    src, logits, grad = z.clone(), torch.empty_like(z), torch.empty_like(z)
+    after = torch.empty(64, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        lpmm.distill_grad(z, ids, t, teacher_lse=lse)
+    torch.cuda.current_stream().wait_stream(side)
+    with torch.cuda.graph(graph):
+        logits.copy_(src)
+        loss, _ = lpmm.distill_grad(logits, ids, t, teacher_lse=lse, out=grad)
+        after.copy_(loss * 2)
+    for k in range(5):
+        src.copy_(z * (1 + k))
+        graph.replay()
+        want, gwant = lpmm.distill_grad(z * (1 + k), ids, t, teacher_lse=lse)
+        assert torch.equal(after, want * 2) and torch.equal(grad, gwant)

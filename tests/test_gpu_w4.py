@@ -166,6 +166,29 @@ def test_product_on_another_stream():
     assert torch.equal(got, want)
 
 
+def test_a_chain_in_a_graph():
+    """Weights requantized, used and taken back within one captured chain: each call waits for the one before it."""
+    w = torch.randn(700, 1000, generator=_gen(8), device="cuda")
+    x = torch.randn(3, 1000, generator=_gen(9), device="cuda")
+    src = w.clone()
+
+    def chain(a):
+        m = lpmm.w4_quantize(a, group=64, zero_points=True)
+        y = lpmm.w4_matvec(m, x)
+        z = lpmm.w4_matvec(m, x * y[:, :1])
+        return y, z, lpmm.w4_dequantize(m, BF16)
+
+    chain(src)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = chain(src)
+    for k in range(6):
+        src.copy_(w * (k - 2.5))
+        graph.replay()
+        for a, b in zip(got, chain(w * (k - 2.5))):
+            assert torch.equal(a, b)
+
+
 # ----------------------------------------------------------------------------------------- quantizer, dequantizer
 
 def _plain_quantize(w, group, zero_points, scale_dtype):
