@@ -512,14 +512,16 @@ __device__ __forceinline__ void load8_bits(const T* row, int c, int cols, bool v
 }
 
 // GB: 32-column blocks per scale (1, 2 or 4; wider groups repeat their scale). NT: tiles of 8 columns of activations.
-template <typename T, int NT, int GB>
-__global__ void __launch_bounds__(kMaxWarps * 32, 1) w4_product_kernel(const W4Product p) {
+// WARPS: 16, or 8 with twice the registers each.
+template <typename T, int NT, int GB, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Product p) {
     using M = typename Operand<T>::M;
     constexpr int PARTS = Operand<T>::parts;
     constexpr int NS = 4 / GB;         // scales per row, stage and lane: the four lanes of a row hold a stage's
     extern __shared__ __align__(128) unsigned char smem[];
     const W4Quant& a = p.w;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int warps = WARPS;
     const int g = lane >> 2, t = lane & 3;
     const int ranks = 1 << p.log_ranks, rank = blockIdx.x & (ranks - 1), cluster = blockIdx.x >> p.log_ranks;
     const int cols = (int)a.cols, all_stages = (cols + kStageCols - 1) / kStageCols;
@@ -811,12 +813,17 @@ ProductPlan plan_product(int64_t rows, int64_t cols, int columns, int64_t blocks
     return best;
 }
 
-template <typename T, int NT, int GB>
+template <typename T, int NT, int GB, int WARPS>
 cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t blocks, cudaStream_t s) {
-    auto kernel = w4_product_kernel<T, NT, GB>;
+    auto kernel = w4_product_kernel<T, NT, GB, WARPS>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.bytes);
     if (e != cudaSuccess) return e;
     return launch_early(kernel, dim3((unsigned)(plan.clusters * plan.ranks), (unsigned)blocks), plan.warps * 32, plan.bytes, plan.ranks, s, p);
+}
+
+template <typename T, int NT, int GB>
+cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t blocks, cudaStream_t s) {
+    return plan.warps == 8 ? launch_product<T, NT, GB, 8>(p, plan, blocks, s) : launch_product<T, NT, GB, 16>(p, plan, blocks, s);
 }
 
 W4Quant pack_args(const W4Matrix& m, const void* w, int64_t stride, int es) {
