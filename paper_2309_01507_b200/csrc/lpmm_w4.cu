@@ -17,7 +17,8 @@ namespace {
 constexpr int kW4Threads = 256;
 constexpr int kW4Warps = kW4Threads / 32;
 constexpr int kLaneCols = 16;     // consecutive columns of a lane = eight bytes of codes: a group's scale, its reciprocal and the
-                                  // addresses are worked out once for them (with eight columns: 196 us instead of XX, see below)
+                                  // addresses are worked out once for them (32000 x 4096 bf16 to codes and back: 153 us,
+                                  // with eight columns 196, both before rows were handled in pieces)
 constexpr int kSpan = 32 * kLaneCols;         // columns that a warp takes at a time
 constexpr int kTmp = kSpan + 32 * 4;          // floats of shared memory to hand them on, with room between the lanes' shares
 
@@ -353,10 +354,10 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
 // y[m, i] = sum over the groups of s (sum over the group's columns of (q - z) x[m, k]): q - z is a small whole number, exact in
 // the 16-bit types, so the inner sums run on the tensor cores (m16n8k16, rows of the weight by tokens, binary32 sums) and a
 // scale is applied once per group to their result. fp32 activations enter as three bfloat16 parts that add up to them exactly
-// (8 significant bits each), as three columns instead of one.
+// (8 significant bits each), one product after the other into the same sums.
 //
 // One CTA per SM holds the activations in shared memory and goes through tiles of 16 rows; its warps share out the stages (16 rows
-// by 512 columns, 4 KB of codes) of all its tiles evenly, in order, each streaming its own through two buffers of its own in shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. The four lanes of a
+// by 512 columns, 4 KB of codes; half as much where the activations need the room) of all its tiles evenly, in order, each streaming its own through two buffers of its own in shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. The four lanes of a
 // row take consecutive quarters of a group's codes, 8 codes = a 32-bit word per product; the pairs that its halves hold, (0, 4), (1, 5), (2, 6), (3, 7), are brought to the tensor
 // cores' operand by a mask and one exact multiply-add. The order of the columns inside a product is free as long as both operands
 // have the same: the activations' pairs are put into that order.
@@ -364,8 +365,6 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
 // A tile's sums from the warps that share it, and from the CTAs of a cluster, which split the columns when the activations do not
 // fit one CTA or the tiles are few, are added in a fixed order at the end: results are the same bits every time.
 
-constexpr int kStageCols = 512, kStageBytes = kStageCols / 2;   // columns of one stage; its bytes per row
-constexpr int kStage = 16 * kStageBytes;                        // 4 KB
 constexpr int kDepth = 2;                                       // stages that a warp holds, the one it works on among them
 constexpr int kXPad = 64;                                       // bytes between columns: neighbouring columns on other banks
 
@@ -462,14 +461,13 @@ struct W4Product {
     int32_t block_tokens;   // tokens of one pass over the codes (blockIdx.y)
     int32_t x_pitch;        // bytes between the activations' columns (tokens, or parts of them) in shared memory
     int32_t tiles, tiles_extra;   // tiles of 16 rows per cluster; the first tiles_extra clusters have one more
-    int32_t log_ranks, log_warps;
+    int32_t log_ranks;
     int32_t log_run;        // threads that take a token's activations while they are put into shared memory (a power of two)
 };
 
-constexpr int kZeroLine = 1024;     // bytes of zeros that are read in place of columns that are not there
 constexpr int kColPitch = 20;      // floats between the columns of 16 sums: the four lanes of a row on different banks
-constexpr int kMaxWarps = 16;
-constexpr int kMaxColumns = 16;    // 32 with half the warps: 4096 x 11008, 32 tokens 72 us, against 48 us with two passes over the codes
+constexpr int kProductWarps = 16, kLogProductWarps = 4;
+constexpr int kMaxTokens = 16;     // columns of activations at a time: two operand tiles, the sums of four do not fit 128 registers
 
 // The warp that has unit u of `units` spread over `warps` (each has [units w / warps, units (w + 1) / warps)).
 __device__ __forceinline__ int warp_of(int u, int units, int warps) { return ((u + 1) * warps - 1) / units; }
@@ -511,40 +509,42 @@ __device__ __forceinline__ void load8_bits(const T* row, int c, int cols, bool v
     }
 }
 
-// GB: 32-column blocks per scale (1, 2 or 4; wider groups repeat their scale). NT: tiles of 8 columns of activations.
-// WARPS: 16, or 8 with twice the registers each.
-template <typename T, int NT, int GB, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Product p) {
+// GB: 32-column blocks per scale (1, 2 or 4; wider groups repeat their scale). NT: tiles of 8 columns of activations. STAGE: columns
+// of a stage, 512 or 256.
+template <typename T, int NT, int GB, int STAGE>
+__global__ void __launch_bounds__(kProductWarps * 32, 1) w4_product_kernel(const W4Product p) {
     using M = typename Operand<T>::M;
     constexpr int PARTS = Operand<T>::parts;
-    constexpr int NS = 4 / GB;         // scales per row, stage and lane: the four lanes of a row hold a stage's
+    constexpr int kStageBytes = STAGE / 2, kStage = 16 * kStageBytes;      // bytes of a row's part of a stage, of a stage
+    constexpr int GROUPS = STAGE / 32 / GB, NS = GROUPS > 4 ? GROUPS / 4 : 1;    // scales of a row per stage, and per lane: its four share them
     extern __shared__ __align__(128) unsigned char smem[];
     const W4Quant& a = p.w;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    constexpr int warps = WARPS;
+    constexpr int warps = kProductWarps;
     const int g = lane >> 2, t = lane & 3;
     const int ranks = 1 << p.log_ranks, rank = blockIdx.x & (ranks - 1), cluster = blockIdx.x >> p.log_ranks;
-    const int cols = (int)a.cols, all_stages = (cols + kStageCols - 1) / kStageCols;
+    const int cols = (int)a.cols, all_stages = (cols + STAGE - 1) / STAGE;
     const int tiles = p.tiles + (cluster < p.tiles_extra), tile0 = cluster * p.tiles + min(cluster, p.tiles_extra);
     const int st0 = all_stages * rank >> p.log_ranks, stages = (all_stages * (rank + 1) >> p.log_ranks) - st0;
     const int units = tiles * stages, sharing = min(warps, units);      // each warp's share, [u0, u1)
-    const int u0 = units > warps ? units * warp >> p.log_warps : min(warp, units), u1 = units > warps ? units * (warp + 1) >> p.log_warps : min(warp + 1, units);
+    const int u0 = units > warps ? units * warp >> kLogProductWarps : min(warp, units), u1 = units > warps ? units * (warp + 1) >> kLogProductWarps : min(warp + 1, units);
     const int first_tile = u0 / stages, first_stage = u0 - first_tile * stages;
     const int64_t m0 = (int64_t)blockIdx.y * p.block_tokens;
-    const int mcount = (int)min((int64_t)p.block_tokens, p.tokens - m0), ncols = mcount * PARTS;
+    const int mcount = (int)min((int64_t)p.block_tokens, p.tokens - m0);
 
     // Shared memory: the warps' buffers (later the CTA's sums), the activations, zeros, the sums of (tile, warp) pairs.
     const uint32_t ring = smem_u32(smem) + warp * (kDepth * kStage);
     const uint32_t xs = smem_u32(smem) + warps * (kDepth * kStage);
     const uint32_t zero_line = xs + p.block_tokens * PARTS * p.x_pitch;
-    float* const sums = reinterpret_cast<float*>(smem + warps * (kDepth * kStage) + p.block_tokens * PARTS * p.x_pitch + kZeroLine);
-    const int slot_floats = p.block_tokens * PARTS * kColPitch;
+    float* const sums = reinterpret_cast<float*>(smem + warps * (kDepth * kStage) + p.block_tokens * PARTS * p.x_pitch + STAGE * 2);
+    const int slot_floats = p.block_tokens * kColPitch;
 
-    // Codes: lane l copies 16 bytes of rows l / 16, l / 16 + 2, ... What lies behind the last row or column is read from the last
-    // one instead: its sums are not used, its activations are zeros.
-    const int last_byte = ((cols + 1) / 2 - 1) & ~15, my_byte = (lane & 15) * 16;
+    // Codes: a lane copies 16 bytes of every so manieth row. What lies behind the last row or column is read from the last one
+    // instead: its sums are not used, its activations are zeros.
+    constexpr int PIECES = kStageBytes / 16, ROWS = 32 / PIECES, COPIES = 16 / ROWS;
+    const int last_byte = ((cols + 1) / 2 - 1) & ~15, my_piece = lane & (PIECES - 1), my_row = lane / PIECES;
     const uint8_t* f_base;
-    uint32_t f_off[8];
+    uint32_t f_off[COPIES];
     int f_tile = tile0 + first_tile, f_st = first_stage, fu = u0;
     uint32_t f_slot = 0;
     const auto fetch_rows = [&] {
@@ -552,24 +552,25 @@ __global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Produ
         const int last = (int)min((int64_t)15, a.rows - 1 - row);
         f_base = a.codes + row * a.codes_stride;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f_off[i] = (uint32_t)min(i * 2 + (lane >> 4), last) * (uint32_t)a.codes_stride;
+        for (int i = 0; i < COPIES; ++i) f_off[i] = (uint32_t)min(i * ROWS + my_row, last) * (uint32_t)a.codes_stride;
     };
     fetch_rows();
     const auto fetch = [&] {
         if (fu < u1) {
-            const uint32_t o = ring + f_slot + (lane >> 4) * kStageBytes;
+            const uint32_t o = ring + f_slot + my_row * kStageBytes;
             f_slot = f_slot == (kDepth - 1) * kStage ? 0 : f_slot + kStage;
-            const uint8_t* const src = f_base + min((st0 + f_st) * kStageBytes + my_byte, last_byte);
+            const uint8_t* const src = f_base + min((st0 + f_st) * kStageBytes + my_piece * 16, last_byte);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(o + i * 2 * kStageBytes + (((lane & 15) ^ row_swizzle(i * 2 + (lane >> 4))) << 4)), "l"(src + f_off[i]) : "memory");
+            for (int i = 0; i < COPIES; ++i)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(o + i * ROWS * kStageBytes + ((my_piece ^ row_swizzle(i * ROWS + my_row)) << 4)), "l"(src + f_off[i]) : "memory");
             if (++f_st == stages) { f_st = 0; ++f_tile; fetch_rows(); }
             ++fu;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
 
-    // Scales (and zero points) of a stage, one stage ahead, in registers: lane t of a row holds groups t NS to t NS + NS - 1.
+    // Scales (and zero points) of a stage, one stage ahead, in registers: lane t of a row holds groups t NS to t NS + NS - 1, or, of
+    // fewer than four, group t mod their number.
     int s_tile = tile0 + first_tile, s_st = first_stage;
     int64_t ra, rb;
     const auto scale_rows = [&] {
@@ -581,7 +582,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Produ
     const auto load_scales = [&](float (&sa)[NS], float (&sb)[NS], float (&za)[NS], float (&zb)[NS]) {
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            int gi = (st0 + s_st) * (4 * NS) + t * NS + i;
+            int gi = (st0 + s_st) * GROUPS + (GROUPS >= 4 ? t * NS + i : t & (GROUPS - 1));
             if (GB == 4 && wide > 1) gi /= wide;
             const bool in = gi < a.groups;
             gi = in ? gi : 0;
@@ -603,14 +604,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Produ
     // are under way at once, and the clusters start at different places, so that they do not all ask the same part of the L2
     // cache at a time. The first loads go out before the codes', behind which they would queue.
     constexpr int BATCH = PARTS == 1 ? 8 : 4;
-    const int eights = stages * (kStageCols / 8), m_step = blockDim.x >> p.log_run, my_m = threadIdx.x >> p.log_run;
+    const int eights = stages * (STAGE / 8), m_step = blockDim.x >> p.log_run, my_m = threadIdx.x >> p.log_run;
     const int shift = cluster * 16 % eights;
     int xe = my_m < mcount ? threadIdx.x & ((1 << p.log_run) - 1) : eights, xm = my_m;
     uint4 xv[BATCH][PARTS == 1 ? 1 : 2];
     const auto x_place = [&] { return xe + shift < eights ? xe + shift : xe + shift - eights; };
     const auto load_x = [&] {
         if (xe >= eights) return;
-        const int k = st0 * kStageCols + x_place() * 8;
+        const int k = st0 * STAGE + x_place() * 8;
 #pragma unroll
         for (int j = 0; j < BATCH; ++j)
             if (xm + j * m_step < mcount) load8_bits(static_cast<const T*>(a.w) + (m0 + xm + j * m_step) * a.w_stride, k, cols, a.vec, xv[j]);
@@ -639,7 +640,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Produ
     if (u0 < u1) load_scales(sa, sb, za, zb);
 #pragma unroll
     for (int i = 0; i < kDepth - 1; ++i) fetch();
-    for (int i = threadIdx.x; i < kZeroLine / 16; i += blockDim.x) sts128(zero_line + i * 16, make_uint4(0, 0, 0, 0));
+    for (int i = threadIdx.x; i < STAGE * 2 / 16; i += blockDim.x) sts128(zero_line + i * 16, make_uint4(0, 0, 0, 0));
     while (xe < eights) {
         store_x();
         xm += BATCH * m_step;
@@ -651,12 +652,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Produ
     }
     __syncthreads();
 
-    uint32_t xcol[NT], xstep[NT];
+    uint32_t xcol[NT], xstep[NT], xpart[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const bool in = n * 8 + g < ncols;
-        xcol[n] = (in ? xs + (n * 8 + g) * p.x_pitch : zero_line) + t * 16;
-        xstep[n] = in ? kStageCols * 2 : 0;
+        const bool in = n * 8 + g < mcount;
+        xcol[n] = (in ? xs + (n * 8 + g) * PARTS * p.x_pitch : zero_line) + t * 16;
+        xstep[n] = in ? STAGE * 2 : 0;
+        xpart[n] = in ? p.x_pitch : 0;
     }
     float2 acc[NT][2];      // rows g and g + 8, columns 2t and 2t + 1
 #pragma unroll
@@ -664,7 +666,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Produ
     uint32_t z0 = 0, z0x = 0, z1 = 0, z1x = 0;
     Codes<M>::zero_operand(8.0f, z0, z0x);
     z1 = z0; z1x = z0x;
+    const auto put = [&](int m, int64_t row, float v) {
+        v *= 1.0f / Codes<M>::unit;
+        if (p.bias) v += p.bias[row];
+        const int64_t o = (m0 + m) * p.y_stride + row;
+        if (p.y_f32) static_cast<float*>(p.y)[o] = v;
+        else static_cast<T*>(p.y)[o] = from_f32<T>(v);
+    };
     int tile = first_tile, st = first_stage;
+    bool began = st == 0;       // this warp has the tile's first stage
     uint32_t slot = 0;
     for (int u = u0; u < u1; ++u) {
         fetch();
@@ -674,16 +684,18 @@ __global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Produ
         if (u + 1 < u1) load_scales(nsa, nsb, nza, nzb);
         const uint32_t codes = (ring + slot + g * kStageBytes + t * (4 * GB)) ^ (row_swizzle(g) << 4);
         slot = slot == (kDepth - 1) * kStage ? 0 : slot + kStage;
-        uint32_t xa[NT];
+        uint32_t xa[NT][PARTS];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) xa[n] = xcol[n] + st * xstep[n];
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) xa[n][i] = xcol[n] + st * xstep[n] + i * xpart[n];
         float part[NT][4];
         float s0 = 0.0f, s1 = 0.0f;
         uint32_t wa[GB], wb[GB];
 #pragma unroll
-        for (int b = 0; b < kStageCols / 32; ++b) {
+        for (int b = 0; b < STAGE / 32; ++b) {
             if (b % GB == 0) {        // a new group
-                const int from = (lane & ~3) | (b / 4), i = (b / GB) % NS;
+                const int from = (lane & ~3) | (b / GB / NS), i = (b / GB) % NS;
                 s0 = __shfl_sync(0xffffffffu, sa[i], from);
                 s1 = __shfl_sync(0xffffffffu, sb[i], from);
                 if (a.zeros) {
@@ -701,10 +713,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Produ
             const uint32_t a0[4] = {qa[0], qb[0], qa[1], qb[1]}, a1[4] = {qa[2], qb[2], qa[3], qb[3]};
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const uint4 x = lds128(xa[n] + b * 64);
-                if (b % GB == 0) Codes<M>::mma0(part[n], a0, x.x, x.y);
-                else Codes<M>::mma(part[n], a0, x.x, x.y);
-                Codes<M>::mma(part[n], a1, x.z, x.w);
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) {
+                    const uint4 x = lds128(xa[n][i] + b * 64);
+                    if (b % GB == 0 && i == 0) Codes<M>::mma0(part[n], a0, x.x, x.y);
+                    else Codes<M>::mma(part[n], a0, x.x, x.y);
+                    Codes<M>::mma(part[n], a1, x.z, x.w);
+                }
             }
             if (b % GB == GB - 1) {
                 const float2 s00 = splat(s0), s11 = splat(s1);
@@ -718,112 +733,119 @@ __global__ void __launch_bounds__(WARPS * 32, 1) w4_product_kernel(const W4Produ
 #pragma unroll
         for (int i = 0; i < NS; ++i) { sa[i] = nsa[i]; sb[i] = nsb[i]; za[i] = nza[i]; zb[i] = nzb[i]; }
         __syncwarp();       // the stage may be overwritten
-        if (++st == stages || u + 1 == u1) {     // (tile, warp) pairs come in order, each raising one of the two: tile + warp numbers them
-            float* const out = sums + (tile + warp) * slot_floats + g;
+        if (++st == stages || u + 1 == u1) {
+            if (ranks == 1 && st == stages && began) {        // all of the tile was this warp's
+                const int64_t row = (int64_t)(tile0 + tile) * 16 + g;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int col = n * 8 + 2 * t;
-                if (col < ncols) { out[col * kColPitch] = acc[n][0].x; out[col * kColPitch + 8] = acc[n][1].x; }
-                if (col + 1 < ncols) { out[(col + 1) * kColPitch] = acc[n][0].y; out[(col + 1) * kColPitch + 8] = acc[n][1].y; }
-                acc[n][0] = acc[n][1] = splat(0.0f);
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int m = n * 8 + 2 * t + i;
+                        if (m < mcount && row < a.rows) put(m, row, i ? acc[n][0].y : acc[n][0].x);
+                        if (m < mcount && row + 8 < a.rows) put(m, row + 8, i ? acc[n][1].y : acc[n][1].x);
+                    }
+                }
+            } else {
+                // A warp shares at most its first tile with those before it and its last one with those behind: two places per warp.
+                // With other ranks every (tile, warp) pair has one; they come in order, each raising one of the two, so that their
+                // sum numbers them.
+                float* const out = sums + (ranks == 1 ? 2 * warp + began : tile + warp) * slot_floats + g;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int m = n * 8 + 2 * t;
+                    if (m < mcount) { out[m * kColPitch] = acc[n][0].x; out[m * kColPitch + 8] = acc[n][1].x; }
+                    if (m + 1 < mcount) { out[(m + 1) * kColPitch] = acc[n][0].y; out[(m + 1) * kColPitch + 8] = acc[n][1].y; }
+                }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = splat(0.0f);
             st = 0;
             ++tile;
+            began = true;
         }
     }
 
-    // The CTA's sums over the warps that had a part of a tile (and over the parts of fp32 activations), to where the buffers were:
-    // [token][row]. Then every rank adds its share of the rows over the ranks.
+    // Tiles that several warps had a part of are added up: a warp takes a tile, two tokens at a time. With other ranks that goes to
+    // where the buffers were, [token][row], and every rank then adds its share of the rows over the ranks.
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
     float* const total = reinterpret_cast<float*>(smem);
-    const int rows_here = tiles * 16;
-    const int half = lane >> 4;      // a warp takes a tile, two tokens at a time
+    const int rows_here = tiles * 16, half = lane >> 4;
     for (int tl = warp; tl < tiles; tl += warps) {
         const int w0 = warp_of(tl * stages, units, sharing), n = warp_of(tl * stages + stages - 1, units, sharing) - w0 + 1;
-        const float* const from = sums + (tl + w0) * slot_floats + (lane & 15);
-        float* const to = total + tl * 16 + (lane & 15);
+        if (ranks == 1 && n == 1) continue;
+        const float* const from = sums + (ranks == 1 ? 2 * w0 + 1 : tl + w0) * slot_floats + (lane & 15);
+        const int64_t row = (int64_t)(tile0 + tl) * 16 + (lane & 15);
 #pragma unroll 4
         for (int m = half; m < mcount; m += 2) {
-            float v = 0.0f;
-            for (int i = 0; i < n; ++i) {
-#pragma unroll
-                for (int part = 0; part < PARTS; ++part) v += from[i * slot_floats + (m * PARTS + part) * kColPitch];
-            }
-            to[m * rows_here] = v;
+            float v = from[m * kColPitch];
+            for (int i = 1; i < n; ++i) v += from[(ranks == 1 ? 2 * i - 1 : i) * slot_floats + m * kColPitch];
+            if (ranks > 1) total[m * rows_here + tl * 16 + (lane & 15)] = v;
+            else if (row < a.rows) put(m, row, v);
         }
     }
-    if (ranks > 1) asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
-    else __syncthreads();
+    if (ranks == 1) return;
+    asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
     const int r_lo = rows_here * rank >> p.log_ranks, share = (rows_here * (rank + 1) >> p.log_ranks) - r_lo;
     for (int i = threadIdx.x; i < share * mcount; i += blockDim.x) {
         const int m = i / share, r = r_lo + i - m * share;
         const int64_t row = (int64_t)tile0 * 16 + r;
         if (row >= a.rows) continue;
-        const float* const at = total + m * rows_here + r;
-        float v;
-        if (ranks > 1) {
-            float of[8];
+        const uint32_t at = smem_u32(total + m * rows_here + r);
+        float of[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) of[k] = k < ranks ? ld_rank(smem_u32(at), k) : 0.0f;
-            v = of[0];
+        for (int k = 0; k < 8; ++k) of[k] = k < ranks ? ld_rank(at, k) : 0.0f;
+        float v = of[0];
 #pragma unroll
-            for (int k = 1; k < 8; ++k) v += of[k];
-        } else {
-            v = *at;
-        }
-        v *= 1.0f / Codes<M>::unit;
-        if (p.bias) v += p.bias[row];
-        const int64_t o = (m0 + m) * p.y_stride + row;
-        if (p.y_f32) static_cast<float*>(p.y)[o] = v;
-        else static_cast<T*>(p.y)[o] = from_f32<T>(v);
+        for (int k = 1; k < 8; ++k) v += of[k];
+        put(m, row, v);
     }
-    if (ranks > 1) asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
-// How a product is laid out: CTAs per cluster, clusters, warps per CTA, shared memory.
+// How a product is laid out: CTAs per cluster, clusters, columns of a stage, shared memory.
 struct ProductPlan {
-    int ranks, clusters, warps;
+    int ranks, clusters, stage;
     size_t bytes;
     int64_t cost;
 };
 
-// The layout with the fewest stages per CTA (as its busiest warp has them; eight warps take half as long again per stage as
-// sixteen do: 11008 x 4096, eight tokens, 16.4 against 14.3 us) among those that fit, and a little for each cluster's last exchange. Clusters of 1, 2, 4 and 8 that run side by side at one CTA per SM: 148, 74, 33 and 15 on this part.
-ProductPlan plan_product(int64_t rows, int64_t cols, int columns, int64_t blocks) {
+// The layout with the fewest stages per CTA (as its busiest warp has them) among those that fit, and a little for each cluster's
+// last exchange. `columns`: of activations in shared memory. Clusters of 1, 2, 4 and 8 that run side by side at one CTA per SM:
+// 148, 74, 33 and 15 on this part.
+ProductPlan plan_product(int64_t rows, int64_t cols, int tokens, int columns, int64_t blocks) {
     const int side_by_side[4] = {148, 74, 33, 15};
-    const int64_t tiles = (rows + 15) / 16, stages = (cols + kStageCols - 1) / kStageCols, room = 227 * 1024 - 1024;
+    const int64_t tiles = (rows + 15) / 16, room = 226 * 1024, slot = (int64_t)tokens * kColPitch * 4;
     ProductPlan best = {0, 0, 0, 0, INT64_MAX};
-    for (int i = 0; i < 4; ++i) {
-        const int ranks = 1 << i;
-        if (ranks > stages && i) break;
-        const int64_t ns = (stages + ranks - 1) / ranks, slot = (int64_t)columns * kColPitch * 4;
-        for (int warps = kMaxWarps; warps >= 8; warps -= 8) {
-            const int64_t ring = (int64_t)warps * kDepth * kStage, fixed = ring + columns * (ns * kStageCols * 2 + kXPad) + kZeroLine;
-            // tiles whose sums fit, by warp behind the rest and by CTA into the buffers
-            const int64_t fit = std::min((room - fixed) / slot - warps, ring / (columns * 64));
-            if (fixed > room || fit < 1) continue;
-            const int64_t at_a_time = std::max<int64_t>(1, side_by_side[i] / blocks);
-            const int64_t per = std::min((tiles + at_a_time - 1) / at_a_time, fit), clusters = (tiles + per - 1) / per;
-            const int64_t waves = (clusters * blocks + side_by_side[i] - 1) / side_by_side[i];
-            const int64_t cost = waves * ((warps == kMaxWarps ? 2 : 3) * warps * ((per * ns + warps - 1) / warps) + 16 + 8 * i);
-            if (cost < best.cost) best = {ranks, (int)clusters, warps, (size_t)(fixed + (per + warps) * slot), cost};
-        }
+    for (int i = 0; i < 8; ++i) {
+        const int log_ranks = i >> 1, ranks = 1 << log_ranks, stage = i & 1 ? 256 : 512;
+        const int64_t stages = (cols + stage - 1) / stage, ns = (stages + ranks - 1) / ranks;
+        if (ranks > stages && ranks > 1) continue;
+        const int64_t ring = (int64_t)kProductWarps * kDepth * 8 * stage, fixed = ring + columns * (ns * stage * 2 + kXPad) + stage * 2;
+        // Tiles whose sums fit: alone, a warp has two; with other ranks, every warp's part of a tile behind the rest, and the CTA's sums
+        // where the buffers were.
+        const int64_t fit = ranks == 1 ? (fixed + 2 * kProductWarps * slot <= room ? tiles : 0) : std::min((room - fixed) / slot - kProductWarps, ring / (tokens * 64));
+        if (fixed > room || fit < 1) continue;
+        const int64_t at_a_time = std::max<int64_t>(1, side_by_side[log_ranks] / blocks);
+        const int64_t per = std::min((tiles + at_a_time - 1) / at_a_time, fit), clusters = (tiles + per - 1) / per;
+        const int64_t waves = (clusters * blocks + side_by_side[log_ranks] - 1) / side_by_side[log_ranks];
+        const int64_t cost = waves * ((stage == 512 ? 20 : 12) * kProductWarps * ((per * ns + kProductWarps - 1) / kProductWarps) + 160 + 80 * log_ranks);
+        if (cost < best.cost) best = {ranks, (int)clusters, stage, (size_t)(fixed + (ranks == 1 ? 2 * kProductWarps : per + kProductWarps) * slot), cost};
     }
     return best;
 }
 
-template <typename T, int NT, int GB, int WARPS>
+template <typename T, int NT, int GB, int STAGE>
 cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t blocks, cudaStream_t s) {
-    auto kernel = w4_product_kernel<T, NT, GB, WARPS>;
+    auto kernel = w4_product_kernel<T, NT, GB, STAGE>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.bytes);
     if (e != cudaSuccess) return e;
-    return launch_early(kernel, dim3((unsigned)(plan.clusters * plan.ranks), (unsigned)blocks), plan.warps * 32, plan.bytes, plan.ranks, s, p);
+    return launch_early(kernel, dim3((unsigned)(plan.clusters * plan.ranks), (unsigned)blocks), kProductWarps * 32, plan.bytes, plan.ranks, s, p);
 }
 
 template <typename T, int NT, int GB>
 cudaError_t launch_product(const W4Product& p, const ProductPlan& plan, int64_t blocks, cudaStream_t s) {
-    return plan.warps == 8 ? launch_product<T, NT, GB, 8>(p, plan, blocks, s) : launch_product<T, NT, GB, 16>(p, plan, blocks, s);
+    return plan.stage == 256 ? launch_product<T, NT, GB, 256>(p, plan, blocks, s) : launch_product<T, NT, GB, 512>(p, plan, blocks, s);
 }
 
 W4Quant pack_args(const W4Matrix& m, const void* w, int64_t stride, int es) {
@@ -832,8 +854,8 @@ W4Quant pack_args(const W4Matrix& m, const void* w, int64_t stride, int es) {
             m.group == 32 ? 5 : m.group == 64 ? 6 : m.group == 128 ? 7 : -1, 1.0f};
 }
 
-// Lays `spans` spans per row out over the grid it returns: 64 CTAs per SM, or as many as there is work for (eight per
-// SM, all resident: XX us).
+// Lays `spans` spans per row out over the grid it returns: 64 CTAs per SM, or as many as there is work for (32000 x 4096
+// fp32: 94 us to codes and 98 back; with eight per SM, all resident, 100 and 105).
 int walk_spans(W4Quant& a, int64_t spans) {
     const int64_t ctas = std::min<int64_t>((a.rows * spans + kW4Warps - 1) / kW4Warps, 148 * 64), warps = ctas * kW4Warps;
     a.spans = (int)spans;
@@ -883,25 +905,24 @@ cudaError_t launch_w4_matvec(const W4Matrix& m, const void* x, int x_dtype, int6
         p.tokens = tokens; p.bias = bias; p.y = y; p.y_stride = y_stride;
         p.scale_dtype = m.scale_dtype;
         p.y_f32 = y_dtype == 0;
-        // Up to 16 columns of activations at a time (a token is PARTS of them), as few as fit beside the rings.
-        int64_t block = std::min<int64_t>(tokens, kMaxColumns / PARTS), blocks;
+        // Up to 16 tokens at a time, as few as fit beside the buffers.
+        int64_t block = std::min<int64_t>(tokens, kMaxTokens), blocks;
         ProductPlan plan;
         for (;; block = (block + 1) / 2) {
             blocks = std::min<int64_t>((tokens + block - 1) / block, 65535);
-            plan = plan_product(m.rows, m.cols, (int)block * PARTS, blocks);
+            plan = plan_product(m.rows, m.cols, (int)block, (int)block * PARTS, blocks);
             if (plan.ranks || block == 1) break;
         }
         if (!plan.ranks) return cudaErrorInvalidConfiguration;      // cannot be: see LPMM_W4_MAX_COLS
         block = std::min(block, (tokens + blocks - 1) / blocks);    // even blocks
         p.block_tokens = (int)block;
-        const int64_t ns = ((m.cols + kStageCols - 1) / kStageCols + plan.ranks - 1) / plan.ranks;
-        p.x_pitch = (int)(ns * kStageCols * 2 + kXPad);
+        const int64_t ns = ((m.cols + plan.stage - 1) / plan.stage + plan.ranks - 1) / plan.ranks;
+        p.x_pitch = (int)(ns * plan.stage * 2 + kXPad);
         const int64_t tiles = (m.rows + 15) / 16;
         p.tiles = (int)(tiles / plan.clusters);
         p.tiles_extra = (int)(tiles % plan.clusters);
         while (1 << p.log_ranks < plan.ranks) ++p.log_ranks;
-        while (1 << p.log_warps < plan.warps) ++p.log_warps;
-        while (1 << p.log_run < ns * (kStageCols / 8) && 1 << p.log_run < plan.warps * 32) ++p.log_run;
+        while (1 << p.log_run < ns * (plan.stage / 8) && 1 << p.log_run < kProductWarps * 32) ++p.log_run;
         const auto run = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
             // grid.y counts blocks of tokens and ends at 65535; the rest is another launch's
@@ -916,8 +937,7 @@ cudaError_t launch_w4_matvec(const W4Matrix& m, const void* x, int x_dtype, int6
             }
             return cudaSuccess;
         };
-        const int64_t columns = block * PARTS;
-        if (columns <= 8) return run(std::integral_constant<int, 1>{});
+        if (block <= 8) return run(std::integral_constant<int, 1>{});
         return run(std::integral_constant<int, 2>{});
     });
 }

@@ -95,7 +95,8 @@ def test_product_groups_and_scales(group, scale_dtype, zeros):
             _check_product(m, x, lpmm.w4_matvec(m, x))
 
 
-@pytest.mark.parametrize("rows,cols,tokens", [(4096, 4096, 1), (32000, 4096, 1), (11008, 4096, 8), (4096, 11008, 32), (50265, 1024, 3), (5, 100003, 2), (70001, 33, 2)])
+@pytest.mark.parametrize("rows,cols,tokens", [(4096, 4096, 1), (32000, 4096, 1), (11008, 4096, 8), (4096, 11008, 32), (50265, 1024, 3), (5, 100003, 2), (70001, 33, 2), (11008, 4096, 16), (4096, 11008, 33),
+                                              (1000, 20000, 5), (2500, 131072, 1), (40, 131072, 16)])
 def test_product_of_layers(rows, cols, tokens):
     for dtype in (BF16, F32):
         m = _random_matrix(rows, cols, seed=1)
