@@ -354,7 +354,8 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
 // y[m, i] = sum over the groups of s (sum over the group's columns of (q - z) x[m, k]): q - z is a small whole number, exact in
 // the 16-bit types, so the inner sums run on the tensor cores (m16n8k16, rows of the weight by tokens, binary32 sums) and a
 // scale is applied once per group to their result. fp32 activations enter as three bfloat16 parts that add up to them exactly
-// (8 significant bits each), one product after the other into the same sums.
+// (8 significant bits each), the first into a group's sums, the other two into sums of their own,
+// so that what is small is not cut off at what is large.
 //
 // One CTA per SM holds the activations in shared memory and goes through tiles of 16 rows; its warps share out the stages (16 rows
 // by 512 columns, 4 KB of codes; half as much where the activations need the room) of all its tiles evenly, in order, each streaming its own through two buffers of its own in shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. The four lanes of a
@@ -689,7 +690,7 @@ __global__ void __launch_bounds__(kProductWarps * 32, 1) w4_product_kernel(const
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int i = 0; i < PARTS; ++i) xa[n][i] = xcol[n] + st * xstep[n] + i * xpart[n];
-        float part[NT][4];
+        float part[NT][4], low[NT][4];       // a group's sums; of fp32 activations' lower parts: the tensor cores' additions truncate
         float s0 = 0.0f, s1 = 0.0f;
         uint32_t wa[GB], wb[GB];
 #pragma unroll
@@ -716,17 +717,23 @@ __global__ void __launch_bounds__(kProductWarps * 32, 1) w4_product_kernel(const
 #pragma unroll
                 for (int i = 0; i < PARTS; ++i) {
                     const uint4 x = lds128(xa[n][i] + b * 64);
-                    if (b % GB == 0 && i == 0) Codes<M>::mma0(part[n], a0, x.x, x.y);
-                    else Codes<M>::mma(part[n], a0, x.x, x.y);
-                    Codes<M>::mma(part[n], a1, x.z, x.w);
+                    float (&to)[4] = i == 0 ? part[n] : low[n];
+                    if (b % GB == 0 && i < 2) Codes<M>::mma0(to, a0, x.x, x.y);
+                    else Codes<M>::mma(to, a0, x.x, x.y);
+                    Codes<M>::mma(to, a1, x.z, x.w);
                 }
             }
             if (b % GB == GB - 1) {
                 const float2 s00 = splat(s0), s11 = splat(s1);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    acc[n][0] = fma2_rn(s00, make_float2(part[n][0], part[n][1]), acc[n][0]);
-                    acc[n][1] = fma2_rn(s11, make_float2(part[n][2], part[n][3]), acc[n][1]);
+                    float2 p0 = make_float2(part[n][0], part[n][1]), p1 = make_float2(part[n][2], part[n][3]);
+                    if constexpr (PARTS > 1) {
+                        p0 = add2_rn(p0, make_float2(low[n][0], low[n][1]));
+                        p1 = add2_rn(p1, make_float2(low[n][2], low[n][3]));
+                    }
+                    acc[n][0] = fma2_rn(s00, p0, acc[n][0]);
+                    acc[n][1] = fma2_rn(s11, p1, acc[n][1]);
                 }
             }
         }
