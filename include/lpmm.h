@@ -254,11 +254,12 @@ lpmm_status lpmm_dequantize(const uint8_t* d_codes, const float* d_scale0, const
  * The form in which a trained matrix is put into service: weight (i, k) = (code - zero) * scale with one scale, and
  * optionally one zero point, per `group` consecutive columns of a row (the last group of a row may be shorter).
  *   d_codes  rows x codes_stride bytes; column 2k of a row sits in bits 0-3 of its byte k, column 2k + 1 in bits 4-7.
- *            codes_stride is a multiple of 16 and at least ceil(cols / 2); d_codes is 16-byte aligned. What the bytes behind
+ *            codes_stride is a multiple of 16, at least ceil(cols / 2) and at most 2^27; d_codes is 16-byte aligned. What the bytes behind
  *            a row's last column hold does not matter.
  *   d_scales rows x ceil(cols / group), contiguous, of type scale_dtype (LPMM_F32, LPMM_BF16 or LPMM_F16).
  *   d_zeros  rows x ceil(cols / group) bytes, contiguous, 0 .. 15; NULL: 8 everywhere.
  *   group    32, 64 or a multiple of 128.
+ * rows, cols < 2^30 and rows * cols <= 2^40.
  * All sums are kept in binary32 and every code enters the products exactly. */
 typedef struct {
     uint8_t* d_codes;
@@ -307,7 +308,7 @@ lpmm_status lpmm_w4_matvec(const lpmm_w4* m, const void* d_x, int32_t x_dtype, i
  *   d_loss    tokens floats; d_grad tokens x vocab of the logits' type, rows grad_stride elements apart. d_grad may be
  *             d_logits itself with the same stride (the gradient then replaces the logits); it must not overlap otherwise.
  * 1 <= top <= min(vocab, LPMM_DISTILL_MAX_TOP), vocab <= LPMM_DISTILL_MAX_VOCAB, else LPMM_ERR_UNSUPPORTED; tokens 0:
- * nothing to do. Results do not depend on the launch: they are the same bits every time. */
+ * nothing to do. The same call gives the same bits every time. */
 #define LPMM_DISTILL_MAX_TOP 1024
 #define LPMM_DISTILL_MAX_VOCAB 262144
 lpmm_status lpmm_distill_loss(const void* d_logits, int32_t dtype, int64_t logits_stride, int64_t tokens, int64_t vocab,

@@ -523,7 +523,7 @@ cudaError_t launch(const DistillArgs& a, int log_cluster, int slice_vecs, size_t
 cudaError_t launch_distill(const DistillArgs& a, int logits_dtype, cudaStream_t s) {
     const int64_t es = logits_dtype == 0 ? 4 : 2;
     const int64_t row_vecs = a.vocab * es / 16 + 2;    // however the row is aligned
-    // A CTA takes a whole row where its shared memory holds one; the CTAs of a cluster wait for one another twice per row, which
+    // A CTA takes a whole row where its shared memory holds one; the CTAs of a cluster wait for one another once per row, which
     // costs more than it gains. Few rows are split, until every SM has a CTA or a slice is down to 8 KB.
     int log_cluster = 0;
     const auto slice_of = [&](int l) { return ((row_vecs + (1 << l) - 1) >> l) + 1; };

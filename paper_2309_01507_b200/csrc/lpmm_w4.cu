@@ -458,7 +458,7 @@ template <> struct Codes<__nv_bfloat16> {
 template <typename T> struct Operand { using M = T; static constexpr int parts = 1; };
 template <> struct Operand<float> { using M = __nv_bfloat16; static constexpr int parts = 3; };
 
-// Rows lie 256 bytes apart in a stage; its 16-byte pieces are permuted by the row, so that whatever the lanes of a warp read at a
+// Rows lie 128 or 256 bytes apart in a stage; its 16-byte pieces are permuted by the row, so that whatever the lanes of a warp read at a
 // time (4, 8 or 16 bytes from each of 8, 4 or 2 rows) lies on different banks: the row's three low bits, reversed.
 __device__ __forceinline__ int row_swizzle(int r) { return (r & 1) << 2 | (r & 2) | (r & 4) >> 2; }
 
